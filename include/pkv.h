@@ -342,6 +342,83 @@ int pkv_stream_read_pages(const uint16_t* k_cache, const uint16_t* v_cache, int3
                           int32_t heads_per_workgroup, uint32_t* sink, hipStream_t stream, hipEvent_t start,
                           hipEvent_t stop);
 
+/* ---- 8-bit paged KV cache ---------------------------------------------------------------
+ * A pool that holds K and V in 8 bits with an fp32 scale for each token and KV head, in pages of
+ * 16 tokens under the same block tables: half the bytes of the fp16 pools in HBM and of a decode
+ * step's reads. A pool is uint8 [num_pages, Hkv, pkv_kv8_record_bytes(d)], 16-byte aligned; the
+ * record of a page and KV head holds (4224 bytes at d = 128)
+ *     K codes [16][128], V codes [4][128][4] (token 4a + b, dim c at [a][c][b]),
+ *     K scales fp32 [16], V scales fp32 [16]
+ * and a stored value is code * scale. With m the largest magnitude of the token's 128 values:
+ *     PKV_KV8_INT8  scale = m / 127, code = x * 127 / m rounded to the nearest integer (ties to even)
+ *     PKV_KV8_E4M3  scale = m / 448, code = x * 448 / m rounded to the nearest e4m3 (ties to even)
+ * (the codes are exactly those of real arithmetic; the scale is m / 127 or m / 448 rounded to fp32).
+ * m = 0 gives scale 0. A vector with an infinity or NaN gets scale NaN and codes 0, so all its values
+ * read back as NaN, and attention over it gives NaN.
+ *
+ * Shared by the three calls: d = 128 (else PKV_ERR_UNSUPPORTED); block_table int32 [B,
+ * max_pages_per_row]; seq_lens int32 [B]; ws a workspace set up by pkv_workspace_init for (B, Hkv),
+ * whose error word takes the device error bits (pkv_check_device_status). Two rows' tables may name
+ * the same page (a shared prefix) as long as no call appends to it for more than one of them.
+ * Calls on one stream may share a workspace; captured graphs too, replayed one after another. */
+#define PKV_KV8_INT8 0
+#define PKV_KV8_E4M3 1
+
+/* Bytes of the record of one page and KV head; 0 when d is not supported. */
+size_t pkv_kv8_record_bytes(int32_t d);
+
+/* Bytes of workspace that pkv_kv8_decode needs: header, B * Hkv completion counters, and state
+ * slots whose number does not depend on the lengths. Returns 0 on a bad argument (Hq / Hkv must be
+ * 1 to 8). pkv_kv8_append and pkv_kv8_gather use the header only (256 bytes). */
+size_t pkv_kv8_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
+
+/* Quantise the last tokens of each row into its pages (one kernel).
+ *   k, v      device fp16 [tokens, Hkv, d]; consecutive tokens are k_stride and v_stride halves
+ *             apart (at least Hkv * d, a multiple of 8; 16-byte aligned), so slices of a fused
+ *             projection need no copy
+ *   offsets   device int32 [B+1]: row i's tokens are offsets[i] .. offsets[i+1]-1 of k and v, and
+ *             become the row's last tokens, positions seq_lens[i] - (offsets[i+1] - offsets[i]) ..
+ *             seq_lens[i] - 1. offsets[0] = 0, ascending; tokens from offsets[B] on are not read.
+ *             NULL: one token per row (tokens == B); rows of length 0 are skipped
+ *   tokens    rows of k and v (0: nothing is enqueued)
+ *   cache     device, see above; only the named positions are written
+ *   seq_lens  lengths after the append
+ * A row whose length is out of range or below its token count sets PKV_DEVERR_SEQ_LEN, a page id
+ * outside the pool PKV_DEVERR_PAGE_ID; the tokens concerned are not written. */
+int pkv_kv8_append(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride, const int32_t* offsets,
+                   int32_t tokens, void* cache, int32_t num_pages, const int32_t* block_table,
+                   int32_t max_pages_per_row, const int32_t* seq_lens, int32_t B, int32_t Hkv, int32_t d,
+                   int32_t format, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Read back the last tokens of each row: k and v [tokens, Hkv, d] = fp16(code * scale), with
+ * offsets, tokens, strides and seq_lens as for pkv_kv8_append (any interval of a row can be read:
+ * seq_lens[i] is its end). Without offsets a row of length 0 is written as zeros, and so are
+ * tokens that set an error bit. One kernel. */
+int pkv_kv8_gather(const void* cache, int32_t num_pages, const int32_t* block_table, int32_t max_pages_per_row,
+                   const int32_t* seq_lens, const int32_t* offsets, int32_t tokens, int32_t B, int32_t Hkv, int32_t d,
+                   int32_t format, uint16_t* k, uint16_t* v, int64_t k_stride, int64_t v_stride, void* ws,
+                   size_t ws_bytes, hipStream_t stream);
+
+/* Attention of one token per row over an 8-bit cache (one kernel): Eq. (1) with the stored values
+ * as K and V. The batch's pages are dealt evenly over the device in order of (row, KV head, page),
+ * and the online-softmax states of a (row, KV head) that several workgroups share are merged by the
+ * last of them to finish, in order (Sec. 3.3-3.4); there is nothing to plan or choose.
+ *   q         device fp16 [B, Hq, d], rows q_stride halves apart (at least Hq * d, a multiple of 8;
+ *             16-byte aligned)
+ *   out       device fp16 [B, Hq, d], 16-byte aligned; rows of length 0 are written as zeros
+ *   sm_scale  softmax scale (1/sqrt(d) of Eq. 1 unless Q is pre-scaled)
+ *   ws        at least pkv_kv8_workspace_size(B, Hq, Hkv, d) bytes; its completion counters must be
+ *             zero at launch, and every call leaves them zero
+ * Hq / Hkv from 1 to 8 and B <= 4096, else PKV_ERR_UNSUPPORTED; also when B * Hkv *
+ * (max_pages_per_row / 2 + 2) passes 2^31 - 1. Rows whose length is out of range (PKV_DEVERR_SEQ_LEN)
+ * or that name a page outside the pool (PKV_DEVERR_PAGE_ID) are written as zeros. Scores, softmax
+ * statistics and sums are fp32; the weights enter P.V as two bf16 halves (16 bits). Results do not
+ * depend on anything but the inputs and the device's compute units. */
+int pkv_kv8_decode(const uint16_t* q, int64_t q_stride, const void* cache, int32_t num_pages,
+                   const int32_t* block_table, int32_t max_pages_per_row, const int32_t* seq_lens, int32_t B,
+                   int32_t Hq, int32_t Hkv, int32_t d, int32_t format, float sm_scale, uint16_t* out, void* ws,
+                   size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

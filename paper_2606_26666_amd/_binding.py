@@ -29,6 +29,8 @@ PKV_DEVERR_TASK = 4
 PKV_FUSED_MERGE = 1
 PKV_SPLIT_BATCH = 0
 PKV_SPLIT_QUOTA = 1
+PKV_KV8_INT8 = 0
+PKV_KV8_E4M3 = 1
 TASK_FIELDS = 5  # row, kvh, split, t_begin, t_end
 
 
@@ -46,6 +48,7 @@ class PlanParams(ctypes.Structure):
 
 _lib = None
 _P, _I32, _F32, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+_I64 = ctypes.c_int64
 _SIGS = {
     "pkv_max_tasks": (_I32, [_I32, _I32, _I32]),
     "pkv_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32]),
@@ -77,6 +80,14 @@ _SIGS = {
     "pkv_stream_read_nt_timed": (ctypes.c_int, [_P, _SZ, _P, _P, _P, _P]),
     "pkv_stream_read_pages": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _I32, _I32, _I32, _P, _P, _I32, _I32, _P,
                                              _P, _P, _P]),
+    "pkv_kv8_record_bytes": (_SZ, [_I32]),
+    "pkv_kv8_workspace_size": (_SZ, [_I32, _I32, _I32, _I32]),
+    "pkv_kv8_append": (ctypes.c_int, [_P, _P, _I64, _I64, _P, _I32, _P, _I32, _P, _I32, _P, _I32, _I32, _I32, _I32,
+                                      _P, _SZ, _P]),
+    "pkv_kv8_gather": (ctypes.c_int, [_P, _I32, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _P, _P, _I64, _I64,
+                                      _P, _SZ, _P]),
+    "pkv_kv8_decode": (ctypes.c_int, [_P, _I64, _P, _I32, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32, _F32, _P, _P,
+                                      _SZ, _P]),
 }
 
 
@@ -379,3 +390,136 @@ class DecodeBuffers:
         """The partial-state slots as a byte view (tests fill it with NaN)."""
         off = 256 + ((self.B * self.Hkv * 4 + 255) // 256) * 256
         return self.ws[off:]
+
+
+# ---- 8-bit paged KV cache (see include/pkv.h)
+
+def pkv_kv8_record_bytes(d: int) -> int:
+    return int(lib().pkv_kv8_record_bytes(d))
+
+
+def pkv_kv8_workspace_size(B: int, Hq: int, Hkv: int, d: int) -> int:
+    return int(lib().pkv_kv8_workspace_size(B, Hq, Hkv, d))
+
+
+def _one_device(device: int, stream, **tensors):
+    """The tensors of a call belong on one device, the current one unless a stream is given: a
+    kernel of another device's stream would read memory that is not its own."""
+    for name, t in tensors.items():
+        if t is not None and t.device.index != device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on device {device}")
+    if stream is None and device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _rows(t: torch.Tensor, name: str) -> tuple:
+    """(pointer, halves between tokens) of fp16 [tokens, heads, d] whose heads lie one after another."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype is not torch.float16:
+        raise TypeError(f"{name} must be torch.float16, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, d]")
+    n, heads, d = t.shape
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * d
+
+
+def _pool(cache: torch.Tensor, d: int) -> tuple:
+    ptr = _dev(cache, torch.uint8, "cache")
+    if cache.dim() != 3 or cache.shape[2] != pkv_kv8_record_bytes(d):
+        raise ValueError(f"cache must be [num_pages, Hkv, {pkv_kv8_record_bytes(d)}]")
+    return ptr, cache.shape[0], cache.shape[1]
+
+
+def _table(block_table: torch.Tensor, seq_lens: torch.Tensor) -> tuple:
+    bt, lens = _dev(block_table, torch.int32, "block_table"), _dev(seq_lens, torch.int32, "seq_lens")
+    if block_table.dim() != 2 or seq_lens.dim() != 1 or block_table.shape[0] != seq_lens.shape[0]:
+        raise ValueError("block_table must be [B, max_pages_per_row] and seq_lens [B]")
+    return bt, block_table.shape[1], lens, seq_lens.shape[0]
+
+
+def _offsets(offsets, B: int) -> int:
+    if offsets is None:
+        return 0
+    ptr = _dev(offsets, torch.int32, "offsets")
+    if offsets.numel() != B + 1:
+        raise ValueError("offsets must be [B + 1]")
+    return ptr
+
+
+def pkv_kv8_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor,
+                   seq_lens: torch.Tensor, ws: torch.Tensor, *, format: int, offsets=None, stream=None):
+    """Quantise k, v fp16 [tokens, Hkv, d] (slices of a fused projection are fine) into the pages of
+    their rows, as each row's last tokens; seq_lens are the lengths after it. offsets: int32 [B + 1]
+    into the tokens, or None for one token per row."""
+    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
+    if k.shape != v.shape:
+        raise ValueError("k and v must have one shape")
+    tokens, hkv, d = k.shape
+    cp, num_pages, heads = _pool(cache, d)
+    if heads != hkv:
+        raise ValueError(f"cache holds {heads} KV heads, k has {hkv}")
+    bt, maxp, lens, B = _table(block_table, seq_lens)
+    off, wp = _offsets(offsets, B), _dev(ws, torch.uint8, "ws")
+    _one_device(cache.device.index, stream, k=k, v=v, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
+    _check("pkv_kv8_append", lib().pkv_kv8_append(kp, vp, ks, vs, off, tokens, cp, num_pages, bt, maxp, lens, B, hkv, d,
+                                                  format, wp, ws.numel(), _stream(stream)))
+
+
+def pkv_kv8_gather(cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
+                   v: torch.Tensor, ws: torch.Tensor, *, format: int, offsets=None, stream=None):
+    """Read each row's last tokens back into k, v fp16 [tokens, Hkv, d]; offsets as for
+    pkv_kv8_append. seq_lens[i] is where the interval ends, so any interval can be read."""
+    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
+    if k.shape != v.shape:
+        raise ValueError("k and v must have one shape")
+    tokens, hkv, d = k.shape
+    cp, num_pages, heads = _pool(cache, d)
+    if heads != hkv:
+        raise ValueError(f"cache holds {heads} KV heads, k has {hkv}")
+    bt, maxp, lens, B = _table(block_table, seq_lens)
+    off, wp = _offsets(offsets, B), _dev(ws, torch.uint8, "ws")
+    _one_device(cache.device.index, stream, k=k, v=v, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
+    _check("pkv_kv8_gather", lib().pkv_kv8_gather(cp, num_pages, bt, maxp, lens, off, tokens, B, hkv, d, format, kp, vp,
+                                                  ks, vs, wp, ws.numel(), _stream(stream)))
+
+
+def pkv_kv8_decode(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                   sm_scale: float, out: torch.Tensor, ws: torch.Tensor, *, format: int, stream=None):
+    """Attention of one token per row over an 8-bit cache, in one launch: q, out fp16 [B, Hq, d] (q
+    may be a slice of a fused projection)."""
+    qp, qs = _rows(q, "q")
+    B, hq, d = q.shape
+    cp, num_pages, hkv = _pool(cache, d)
+    bt, maxp, lens, rows = _table(block_table, seq_lens)
+    op, wp = _dev(out, torch.float16, "out"), _dev(ws, torch.uint8, "ws")
+    if rows != B or out.shape != q.shape:
+        raise ValueError("q and out must be [B, Hq, d] with the block table's B")
+    _one_device(cache.device.index, stream, q=q, block_table=block_table, seq_lens=seq_lens, out=out, ws=ws)
+    _check("pkv_kv8_decode", lib().pkv_kv8_decode(qp, qs, cp, num_pages, bt, maxp, lens, B, hq, hkv, d, format,
+                                                  float(sm_scale), op, wp, ws.numel(), _stream(stream)))
+
+
+def kv8_pool(num_pages: int, Hkv: int, d: int, device) -> torch.Tensor:
+    """An empty 8-bit pool of `num_pages` pages."""
+    if pkv_kv8_record_bytes(d) == 0:
+        raise ValueError(f"d = {d} is not supported")
+    return torch.zeros((num_pages, Hkv, pkv_kv8_record_bytes(d)), dtype=torch.uint8, device=device)
+
+
+class Kv8Buffers:
+    """The workspace of the pkv_kv8 calls for batches of B rows."""
+
+    def __init__(self, B: int, Hq: int, Hkv: int, d: int, device):
+        self.B, self.Hq, self.Hkv, self.d = B, Hq, Hkv, d
+        self.ws_bytes = pkv_kv8_workspace_size(B, Hq, Hkv, d)
+        if self.ws_bytes == 0:
+            raise ValueError("bad sizes")
+        self.ws = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
+        pkv_workspace_init(self.ws, B, Hkv)
+
+    def partial_region(self) -> torch.Tensor:
+        """The state slots as a byte view (tests fill it with NaN)."""
+        return self.ws[256 + ((self.B * self.Hkv * 4 + 255) // 256) * 256:]

@@ -272,6 +272,59 @@ inline f4 mfma_f32_k4(float a, float b, f4 c) { return mfma<float, 1>(&a, &b, c)
 #define __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, ...) (emu::wave_sync("mfma operands"), emu::mfma_f16_k16(a, b, c))
 #define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, ...) (emu::wave_sync("mfma operands"), emu::mfma_f32_k4(a, b, c))
 
+// bf16 operands, and the 8-bit formats (OCP e4m3: bias 7, largest 448, 0x7F is NaN).
+namespace emu {
+struct Bf16 {
+  uint16_t b;
+  operator float() const {
+    const uint32_t u = (uint32_t)b << 16;
+    float f;
+    std::memcpy(&f, &u, 4);
+    return f;
+  }
+};
+template <typename V>
+inline f4 mfma_bf16_k32(V a, V b, f4 c) { return mfma<Bf16, 8>(&a, &b, c); }
+inline float from_e4m3(unsigned c) {
+  const int e = (c >> 3) & 15, m = c & 7;
+  const float v = (c & 127) == 127 ? NAN : e == 0 ? std::ldexp((float)m, -9) : std::ldexp((float)(8 + m), e - 10);
+  return c & 128 ? -v : v;
+}
+inline unsigned to_e4m3(float x) {  // nearest, ties to even; beyond the largest: the largest
+  if (std::isnan(x)) return 127;
+  const float a = std::fabs(x);
+  unsigned best = 0;
+  for (unsigned c = 1; c <= 126; ++c) {
+    const float d = std::fabs(from_e4m3(c) - a), b = std::fabs(from_e4m3(best) - a);
+    if (d < b || (d == b && c % 2 == 0)) best = c;
+  }
+  return best | (std::signbit(x) ? 128 : 0);
+}
+}  // namespace emu
+#define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, ...) (emu::wave_sync("mfma operands"), emu::mfma_bf16_k32(a, b, c))
+inline unsigned __builtin_amdgcn_perm(unsigned hi, unsigned lo, unsigned sel) {
+  const uint64_t all = (uint64_t)hi << 32 | lo;
+  unsigned r = 0;
+  for (int i = 0; i < 4; ++i) r |= (unsigned)(all >> (8 * ((sel >> (8 * i)) & 7)) & 255) << (8 * i);
+  return r;
+}
+inline int __builtin_amdgcn_cvt_pk_fp8_f32(float a, float b, int old, bool high) {
+  const unsigned two = emu::to_e4m3(a) | emu::to_e4m3(b) << 8;
+  return high ? (int)(((unsigned)old & 0xFFFFu) | two << 16) : (int)(((unsigned)old & 0xFFFF0000u) | two);
+}
+inline float __builtin_amdgcn_cvt_f32_fp8(int w, int at) { return emu::from_e4m3((unsigned)w >> (8 * at) & 255); }
+inline unsigned __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(unsigned w, float scale, bool high) {
+  unsigned r = 0;
+  for (int i = 0; i < 2; ++i) {
+    const float v = emu::from_e4m3(w >> (16 * high + 8 * i) & 255) * scale;
+    uint32_t u;
+    std::memcpy(&u, &v, 4);
+    r |= (u >> 16) << (16 * i);
+  }
+  return r;
+}
+inline void __builtin_amdgcn_raw_buffer_store_b64(emu::v2 v, __amdgpu_buffer_rsrc_t r, int o, int s, int) { emu::store(v, r, o, s); }
+
 // Transposed LDS read: inside 16 lanes, lane i receives element i % 4 of the four halves that lanes
 // 4 j + i / 4 address, j = 0 .. 3.
 typedef short emu_s4 __attribute__((ext_vector_type(4)));
