@@ -14,6 +14,7 @@ constexpr int P = kPageSize;
 
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
@@ -46,6 +47,12 @@ __device__ __forceinline__ float across_rows(float x, F f) {
   return f(as_f32((unsigned)t[0]), as_f32((unsigned)t[1]));
 }
 
+template <typename F>
+__device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
+  const v2u a = F::load4(lo), b = F::load4(hi);
+  return __builtin_bit_cast(b8v, v4u{a.x, a.y, b.x, b.y});
+}
+
 // ---------------------------------------------------------------------------------
 // Formats. `load8` makes the bf16 operand of eight codes (exact: int8 has 8 and e4m3 4 significant
 // bits); `code` rounds x * top / m, where the product is exact in fp32 (11 + 7 bits) and the
@@ -55,12 +62,69 @@ struct Int8 {
   static constexpr float top = 127.0f;
   static __device__ __forceinline__ unsigned code(float y) { return (unsigned)(int)__builtin_rintf(y) & 255u; }
   static __device__ __forceinline__ float value(unsigned c) { return (float)(signed char)c; }
-  // Two fp32 halves each with an integer of at most 8 bits: their upper 16 bits are the bf16s.
+  // Four codes as bf16: fp32 integers of at most 8 bits, whose upper 16 bits are the bf16s.
   static __device__ __forceinline__ v2u load4(unsigned w) {
+    asm volatile("" : "+v"(w));  // one register: the compiler would carry the masked codes in one each
     const float a = (float)(signed char)(w & 255u), b = (float)(signed char)((w >> 8) & 255u);
     const float c = (float)(signed char)((w >> 16) & 255u), d = (float)(signed char)(w >> 24);
     return v2u{__builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302u), __builtin_amdgcn_perm(as_u32(d), as_u32(c), 0x07060302u)};
   }
+  // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as three
+  // balanced base-256 digits of x = round(q * 2^22 / max|q|), x = 65536 d2 + 256 d1 + d0 with d2 in
+  // [-64, 64], d1 and d0 in [-128, 127]. The sums of digits times codes are exact, and the rounding of
+  // q is 2^-23 of its largest value. First operand: d2 in column h, d1 in column 15 - h; second: d0
+  // in both.
+  struct Query {
+    v4u b[2][2];  // [first, second][half]
+    float unit;   // max|q| * 2^-22 * scale
+    int shift;    // of the own column's sum: 8 for d2, 0 for d1
+    __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
+      unsigned top = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = max(top, max(raw[j][e] & 0x7FFFu, (raw[j][e] >> 16) & 0x7FFFu));
+      top = as_u32(across_rows(as_f32(top), [](float y, float z) { return as_f32(max(as_u32(y), as_u32(z))); }));
+      const float most = there ? (float)__builtin_bit_cast(_Float16, (uint16_t)top) : 0.0f;
+      unit = top < 0x7C00u ? most * 0x1p-22f * scale : __builtin_nanf("");
+      const float inv = most > 0.0f && top < 0x7C00u ? 0x1p22f / most : 0.0f;
+      shift = col < 8 ? 8 : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const h8v y = __builtin_bit_cast(h8v, raw[j]);
+        unsigned first[2] = {0, 0}, second[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int x = inv > 0.0f ? (int)__builtin_rintf((float)y[e] * inv) : 0;
+          const int x1 = (x + 128) >> 8;  // x = 256 x1 + d0
+          const int x2 = (x1 + 128) >> 8;
+          const int d = col < 8 ? x2 : x1;  // d1 and d0: the low bytes of x1 and x
+          first[e >> 2] |= ((unsigned)d & 255u) << (8 * (e & 3));
+          second[e >> 2] |= ((unsigned)x & 255u) << (8 * (e & 3));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          b[0][j >> 1][2 * (j & 1) + i] = first[i];
+          b[1][j >> 1][2 * (j & 1) + i] = second[i];
+        }
+      }
+    }
+    __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
+      v4i c = {0, 0, 0, 0}, c0 = {0, 0, 0, 0};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[0][half]), c, 0, 0, 0);
+        c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[1][half]), c0, 0, 0, 0);
+      }
+      v4f x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = (c[i] << shift) + (dpp<0x140>(c[i]) << (8 - shift));
+        x[i] = __builtin_fmaf((float)t, 256.0f, (float)c0[i]) * (ks[i] * unit);
+      }
+      return x;
+    }
+  };
 };
 struct E4m3 {
   static constexpr float top = 448.0f;
@@ -72,13 +136,35 @@ struct E4m3 {
     return v2u{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
   }
+  // Q.K in bf16: K exactly, a query value as its bf16 high half in column h and low half in column
+  // 15 - h (exact: fp16 has 11 bits); the two columns' sums are added.
+  struct Query {
+    b8v b[4];
+    float unit;
+    __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
+      unit = scale;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const h8v y = __builtin_bit_cast(h8v, raw[j]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f = there ? (float)y[e] : 0.0f;
+          const __bf16 hi = (__bf16)f;
+          b[j][e] = col < 8 ? hi : (__bf16)(f - (float)hi);
+        }
+      }
+    }
+    __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
+      v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<E4m3>(k[j >> 1][2 * (j & 1)], k[j >> 1][2 * (j & 1) + 1]), b[j], x, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (x[i] + mirror16(x[i])) * (ks[i] * unit);
+      return x;
+    }
+  };
 };
-
-template <typename F>
-__device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
-  const v2u a = F::load4(lo), b = F::load4(hi);
-  return __builtin_bit_cast(b8v, v4u{a.x, a.y, b.x, b.y});
-}
 
 // ---------------------------------------------------------------------------------
 // Append and gather.
@@ -200,36 +286,32 @@ __global__ __launch_bounds__(256) void gather_kernel(Kv8MoveArgs a) {
 // Work. A row of n tokens has ceil(n / 32) page pairs for each KV head; a segment is the pairs of
 // one (row, KV head) plus kSegment units for its start and end. Segments lie one after another in
 // order of (row, head), and the units of them all are dealt evenly to the waves of the launch, so
-// no wave has more to read than another whatever the lengths are. A wave runs through its units
-// with one online-softmax state at a time. A segment that lies within one wave goes straight to
-// the output; a state that ends or begins at another wave meets the others of its segment in LDS,
-// and what crosses workgroups goes to the workspace, where the last workgroup to arrive merges.
+// no wave has more to read than another whatever the lengths are. A wave runs through its pairs
+// as one stream, two of them in flight, with one online-softmax state at a time. A segment that
+// lies within one wave goes straight to the output; a state that ends or begins at another wave
+// meets the others of its segment in LDS, and what crosses workgroups goes to the workspace, where
+// the last workgroup to arrive merges.
 //
-// A pair on the matrix cores. K S^T: A = 16 tokens of a page by 32 dims, B = the queries as bf16
-// high and low halves (exact: fp16 has 11 bits), head h in column h and its low half in column
-// 15 - h; the two columns are added by a mirror of the 16 lanes. The result has lane (grp, col) =
-// (lane / 16, lane % 16) holding tokens 4 grp .. 4 grp + 3 of head col: the layout that the second
-// product's B operand has, so the weights go from one product to the next without leaving their
-// lanes. P V: A = V^T, 16 dims by the pair's 32 tokens, B = the weights (times the tokens' V scales)
+// A pair on the matrix cores. S^T = K Q^T: A = 16 tokens of a page, B = the queries, head h in
+// columns h and 15 - h (see the formats). The result has lane (grp, col) = (lane / 16, lane % 16)
+// holding tokens 4 grp .. 4 grp + 3 of its column's head: the layout that the second product's B
+// operand has, so the weights go from one product to the next without leaving their lanes.
+// P V: A = V^T, 16 dims by the pair's 32 tokens, B = the weights (times the tokens' V scales)
 // as bf16 high halves in column h and low halves in column 15 - h. The record's V layout gives each
 // lane its four tokens of eight dims as whole dwords, and K is token-major: codes go from HBM into
-// registers and from there, converted, into the matrix cores, without LDS.
+// registers and from there into the matrix cores, without LDS.
 constexpr int W = 8;        // waves of a workgroup
 constexpr int kSegment = 1;  // units of a segment beyond its pairs
+constexpr int kIdPairs = 32;  // page pairs whose ids a wave holds (one id a lane)
 
 struct Pair {
   v4u k[2][2], v[2][2];  // [page][half]
   v4f ks[2], vs[2];
 };
 
-// State of one segment in a wave: head col < G (col >= 8: the low halves' sums).
-struct State {
-  v4f acc[8];  // tile t, dims 16 grp + .. (see write_state)
-  float m, l;
-};
-
 struct Lds {
-  int pre[kMaxPlanBatch + 1];
+  int pre[kMaxPlanBatch + 1];  // units before each row, for one KV head
+  int len[kMaxPlanBatch];
   int wave_sum[W];
   int seg[2 * W];    // segment of each wave's partial states (-1: none): one it continues, one it begins
   int group_at[2 * W], group_n[2 * W];
@@ -238,6 +320,11 @@ struct Lds {
 };
 
 __device__ __forceinline__ int pairs_of(int len) { return (int)(((unsigned)len + 2 * P - 1) / (2 * P)); }
+
+// The part of a segment that a wave has: pairs p0 .. p1 - 1 of `pairs`.
+struct Segment {
+  int row, head, p0, p1, pairs, len;
+};
 
 template <typename F>
 __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) {
@@ -248,19 +335,19 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   const int slot = G * D + ((2 * G + 3) / 4) * 4;  // floats of a state: acc [G][D], then (m, l) of each head
 
   // Lengths -> units before each row (for one KV head). A length out of range counts as none.
-  const int per = (a.B + W * 64 - 1) / (W * 64);
-  auto length = [&](int i) {
-    const int n = a.seq_lens[i];
-    return n < 0 || n > a.max_pages_per_row * P ? 0 : n;
-  };
   {
+    const int per = (a.B + W * 64 - 1) / (W * 64);
     int sum = 0;
     for (int j = 0; j < per; ++j) {
       const int i = tid * per + j;
       if (i >= a.B) break;
-      const int n = a.seq_lens[i];
-      if (blockIdx.x == 0 && (n < 0 || n > a.max_pages_per_row * P)) atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
-      sum += pairs_of(length(i)) + kSegment;
+      int n = a.seq_lens[i];
+      if (n < 0 || n > a.max_pages_per_row * P) {
+        if (blockIdx.x == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
+        n = 0;
+      }
+      s.len[i] = n;
+      sum += pairs_of(n) + kSegment;
     }
     int run = sum;
 #pragma unroll
@@ -277,7 +364,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       const int i = tid * per + j;
       if (i >= a.B) break;
       s.pre[i] = at;
-      at += pairs_of(length(i)) + kSegment;
+      at += pairs_of(s.len[i]) + kSegment;
       if (i == a.B - 1) s.pre[a.B] = at;
     }
   }
@@ -293,24 +380,12 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   };
   if ((int)blockIdx.x * W >= nw) return;
 
-  // A finished state: out of this wave's registers into `out`.
-  State st;
-  bool bad = false;
-  auto total_l = [&] { return across_rows(st.l, [](float x, float y) { return x + y; }); };
-  auto halves = [&] {  // the low halves' sums join those of the high halves
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st.acc[t][i] += mirror16(st.acc[t][i]);
-  };
-  // Tile t, row 4 grp + i of the products is dim 16 grp + 4 i + t (t < 4) or 64 + 16 grp + 4 i + t - 4.
-
   const int gw = uniform((int)blockIdx.x * W + wave);
   if (gw < nw) {
+    // ---- the wave's segments, one after another
     int u = begin_of(gw);
     const int u_end = begin_of(gw + 1);
-    // the row of unit u
-    int row;
+    int row, head, off;
     {
       const int x = u / a.Hkv;
       int lo = 0, hi = a.B;  // pre[lo] <= x < pre[hi]
@@ -319,193 +394,233 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
         if (s.pre[mid] <= x) lo = mid; else hi = mid;
       }
       row = uniform(lo);
+      const int c = uniform(s.pre[row + 1] - s.pre[row]);
+      const int rel = u - uniform(s.pre[row]) * a.Hkv;
+      head = rel / c;
+      off = rel - head * c;
     }
-    int c_units = uniform(s.pre[row + 1] - s.pre[row]);
-    int rel = u - uniform(s.pre[row]) * a.Hkv;
-    int head = rel / c_units;
-    int off = rel - head * c_units;
-    while (u < u_end) {
-      const int pairs = c_units - kSegment;
-      const int n_units = min(c_units - off, u_end - u);
-      const int p0 = off, p1 = min(off + n_units, pairs);
-      const int len = uniform(length(row));
-      uint16_t* out = a.out + ((size_t)row * a.Hq + (size_t)head * G) * D;
-      if (pairs == 0) {
-        if (off == 0)
-          for (int j = lane; j < G * D / 8; j += 64) reinterpret_cast<v4u*>(out)[j] = v4u{0, 0, 0, 0};
-      } else if (p0 < p1) {
-        // ---- the segment's queries
-        const int myhead = col < 8 ? col : 15 - col;
-        v4u qraw[4];
-        {
-          const uint16_t* q = a.q + (size_t)row * a.q_stride + ((size_t)head * G + (myhead < G ? myhead : 0)) * D + grp * 16;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) qraw[j] = *reinterpret_cast<const v4u*>(q + (j >> 1) * 64 + (j & 1) * 8);
+    auto out_of = [&](const Segment& g) { return a.out + ((size_t)g.row * a.Hq + (size_t)g.head * G) * D; };
+    // The next segment with pairs in the wave's range; empty rows on the way are written as zeros.
+    auto next_segment = [&](Segment& g) __attribute__((always_inline)) {
+      while (u < u_end) {
+        const int len = uniform(s.len[row]), pairs = pairs_of(len);
+        const int n = min(pairs + kSegment - off, u_end - u);
+        g = Segment{row, head, off, min(off + n, pairs), pairs, len};
+        const bool first = off == 0;
+        u += n;
+        off = 0;
+        if (++head == a.Hkv) {
+          head = 0;
+          ++row;
         }
-        // ---- page ids, 64 at a time, the next 64 ahead
-        const int pages = (len + P - 1) / P;
-        const int* table = a.block_table + (size_t)row * a.max_pages_per_row;
-        auto fetch_ids = [&](int pair) { return 2 * pair + lane < pages ? table[2 * pair + lane] : 0; };
-        int ids = fetch_ids(p0), ids_next = fetch_ids(p0 + 32);
-        auto load = [&](Pair& b, int pair) __attribute__((always_inline)) {
-          const int j = pair - p0;
-          if (j > 0 && (j & 31) == 0) {
-            ids = ids_next;
-            ids_next = fetch_ids(pair + 32);
-          }
-#pragma unroll
-          for (int pg = 0; pg < 2; ++pg) {
-            int id = __builtin_amdgcn_readlane(ids, 2 * (j & 31) + (2 * pair + pg < pages ? pg : 0));
-            if (id < 0 || id >= a.num_pages) {
-              bad = true;
-              id = 0;
-            }
-            const uint8_t* rec = a.cache + ((size_t)id * a.Hkv + head) * kKv8Record;
-            const v4u* kp = reinterpret_cast<const v4u*>(rec + col * D + grp * 16);
-            const v4u* vp = reinterpret_cast<const v4u*>(rec + kKv8CodeBytes + grp * (4 * D) + col * 16);
-            const v4f* sp = reinterpret_cast<const v4f*>(rec + kKv8ScaleAt + grp * 16);
-            b.k[pg][0] = __builtin_nontemporal_load(kp);
-            b.k[pg][1] = __builtin_nontemporal_load(kp + 4);
-            b.v[pg][0] = __builtin_nontemporal_load(vp);
-            b.v[pg][1] = __builtin_nontemporal_load(vp + 16);
-            b.ks[pg] = __builtin_nontemporal_load(sp);
-            b.vs[pg] = __builtin_nontemporal_load(sp + 4);
-          }
-        };
-        bad = false;
-        Pair b0, b1;
-        load(b0, p0);
-        if (p0 + 1 < p1) load(b1, p0 + 1);
-        b8v q[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const h8v x = __builtin_bit_cast(h8v, qraw[j]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float f = myhead < G ? (float)x[e] : 0.0f;
-            const __bf16 hi = (__bf16)f;
-            q[j][e] = col < 8 ? hi : (__bf16)(f - (float)hi);
-          }
-        }
-        st.m = kLowest;
-        st.l = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) st.acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        if (pairs == 0 && first)
+          for (int j = lane; j < G * D / 8; j += 64) reinterpret_cast<v4u*>(out_of(g))[j] = v4u{0, 0, 0, 0};
+        if (g.p0 < g.p1) return true;
+      }
+      return false;
+    };
 
-        auto attend = [&](Pair& b, int pair) __attribute__((always_inline)) {
-          v4f x[2];
+    // ---- the load cursor: at most one segment ahead of the one being computed
+    Segment ls, cs;
+    int lp = 0;             // next pair of ls to load
+    int ids = 0, ids_next = 0, ids_p = 0;  // ids of ls's pairs ids_p ..
+    int tag_row = -1, tag_p = 0;           // what ids_next holds
+    bool bad = false, bad_before = false;  // a bad page in ls; in cs when ls is ahead of it
+    bool ahead = false;                    // ls is not cs
+    v4u qraw[4];
+    const int myhead = col < 8 ? col : 15 - col;
+    auto fetch_ids = [&](int r, int p) {
+      tag_row = r;
+      tag_p = p;
+      return 2 * p + lane < a.max_pages_per_row ? a.block_table[(size_t)r * a.max_pages_per_row + 2 * p + lane] : 0;
+    };
+    auto enter_ids = [&](int p) __attribute__((always_inline)) {
+      if (tag_row != ls.row || tag_p != p) ids_next = fetch_ids(ls.row, p);
+      ids = ids_next;
+      ids_p = p;
+      // what comes next: this segment's next pairs, or the next segment's first (of the next row, if
+      // that is not an empty one)
+      if (p + kIdPairs < ls.p1) ids_next = fetch_ids(ls.row, p + kIdPairs);
+      else if (u < u_end) ids_next = fetch_ids(row, 0);
+    };
+    auto enter_segment = [&]() __attribute__((always_inline)) {
+      if (!next_segment(ls)) return false;
+      lp = ls.p0;
+      bad = false;
+      const uint16_t* q = a.q + (size_t)ls.row * a.q_stride + ((size_t)ls.head * G + (myhead < G ? myhead : 0)) * D + grp * 16;
 #pragma unroll
-          for (int pg = 0; pg < 2; ++pg) {
-            x[pg] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < 4; ++j) qraw[j] = *reinterpret_cast<const v4u*>(q + (j >> 1) * 64 + (j & 1) * 8);
+      enter_ids(lp);
+      return true;
+    };
+    auto load_pair = [&](Pair& b) __attribute__((always_inline)) {
+      if (lp - ids_p == kIdPairs) enter_ids(lp);
+      const int pages = (ls.len + P - 1) / P;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const v4u& kk = b.k[pg][j >> 1];
-              x[pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<F>(kk[2 * (j & 1)], kk[2 * (j & 1) + 1]), q[j], x[pg], 0, 0, 0);
+      for (int pg = 0; pg < 2; ++pg) {
+        int id = __builtin_amdgcn_readlane(ids, 2 * (lp - ids_p) + (2 * lp + pg < pages ? pg : 0));
+        if (id < 0 || id >= a.num_pages) {
+          bad = true;
+          id = 0;
+        }
+        const uint8_t* rec = a.cache + ((size_t)id * a.Hkv + ls.head) * kKv8Record;
+        const v4u* kp = reinterpret_cast<const v4u*>(rec + col * D + grp * 16);
+        const v4u* vp = reinterpret_cast<const v4u*>(rec + kKv8CodeBytes + grp * (4 * D) + col * 16);
+        const v4f* sp = reinterpret_cast<const v4f*>(rec + kKv8ScaleAt + grp * 16);
+        b.k[pg][0] = __builtin_nontemporal_load(kp);
+        b.k[pg][1] = __builtin_nontemporal_load(kp + 4);
+        b.ks[pg] = __builtin_nontemporal_load(sp);
+        b.v[pg][0] = __builtin_nontemporal_load(vp);
+        b.v[pg][1] = __builtin_nontemporal_load(vp + 16);
+        b.vs[pg] = __builtin_nontemporal_load(sp + 4);
+      }
+      ++lp;
+    };
+    // Whether a pair was left to load.
+    auto load = [&](Pair& b) __attribute__((always_inline)) {
+      if (lp == ls.p1) {
+        const bool before = bad;
+        if (!enter_segment()) return false;
+        bad_before = before;
+        ahead = true;
+      }
+      load_pair(b);
+      return true;
+    };
+
+    // ---- the segment being computed
+    typename F::Query q;
+    v4f acc[8];  // tile t, row 4 grp + i: dim 16 grp + 4 i + t (t < 4) or 64 + 16 grp + 4 i + t - 4
+    float m, l;
+    int cp;
+    auto begin_segment = [&]() __attribute__((always_inline)) {
+      cs = ls;
+      ahead = false;
+      cp = cs.p0;
+      q.set(qraw, myhead < G, col, a.scale_log2);
+      m = kLowest;
+      l = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    auto end_segment = [&]() __attribute__((always_inline)) {
+      const bool wrong = ahead ? bad_before : bad;
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[t][i] += mirror16(acc[t][i]);  // the low halves' sums join
+      const float sum = across_rows(l, [](float x, float y) { return x + y; });
+      const bool begins = cs.p0 == 0, ends = cs.p1 == cs.pairs;
+      if (wrong && lane == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_PAGE_ID);
+      if (begins && ends) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t* out = out_of(cs);
+        if (col < G) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              h8v o;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = (_Float16)(wrong ? 0.0f : acc[4 * half + (e & 3)][2 * j + (e >> 2)] * inv);
+              *reinterpret_cast<h8v*>(out + col * D + half * 64 + grp * 16 + j * 8) = o;
             }
-          }
+        }
+      } else {
+        const int at = 2 * wave + (begins ? 1 : 0);
+        float* part = s.part + at * slot;
+        if (col < G) {
 #pragma unroll
-          for (int pg = 0; pg < 2; ++pg)
+          for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[pg][i] = (x[pg][i] + mirror16(x[pg][i])) * (b.ks[pg][i] * a.scale_log2);
-          const int left = len - pair * 2 * P;
-          if (left < 2 * P) {  // tokens past the row's end: no weight, whatever the record holds there
-#pragma unroll
-            for (int pg = 0; pg < 2; ++pg) {
-              const int n = min(max(left - pg * P - 4 * grp, 0), 4);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                x[pg][i] = i < n ? x[pg][i] : -__builtin_inff();
-                b.vs[pg][i] = i < n ? b.vs[pg][i] : 0.0f;
-              }
-              const unsigned keep = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
-#pragma unroll
-              for (int h = 0; h < 2; ++h) b.v[pg][h] &= v4u{keep, keep, keep, keep};
-            }
-          }
-          float m = st.m;
-#pragma unroll
-          for (int pg = 0; pg < 2; ++pg)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m = fmaxf(m, x[pg][i]);
-          m = across_rows(m, [](float y, float z) { return fmaxf(y, z); });
-          if (__builtin_amdgcn_ballot_w64(m > st.m) != 0) {
-            const float c = ex2(st.m - m);
-            st.l *= c;
-#pragma unroll
-            for (int t = 0; t < 8; ++t) st.acc[t] *= v4f{c, c, c, c};
-            st.m = m;
-          }
-          b8v w;
-#pragma unroll
-          for (int pg = 0; pg < 2; ++pg)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float e = ex2(x[pg][i] - st.m);
-              st.l += e;
-              const float f = e * b.vs[pg][i];
-              const __bf16 hi = (__bf16)f;
-              w[4 * pg + i] = col < 8 ? hi : (__bf16)(f - (float)hi);
-            }
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-            st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<F>(b.v[0][t >> 2][t & 3], b.v[1][t >> 2][t & 3]), w, st.acc[t], 0, 0, 0);
-        };
-        for (int pair = p0; pair < p1; pair += 2) {
-          attend(b0, pair);
-          if (pair + 2 < p1) load(b0, pair + 2);
-          if (pair + 1 < p1) {
-            attend(b1, pair + 1);
-            if (pair + 3 < p1) load(b1, pair + 3);
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<v4f*>(part + col * D + half * 64 + grp * 16 + i * 4) =
+                  v4f{acc[4 * half][i], acc[4 * half + 1][i], acc[4 * half + 2][i], acc[4 * half + 3][i]};
+          if (grp == 0) {
+            part[G * D + 2 * col] = m;
+            part[G * D + 2 * col + 1] = wrong ? -1.0f : sum;
           }
         }
-
-        // ---- the end of the wave's part of the segment
-        halves();
-        const float l = total_l();
-        const bool begins = p0 == 0, ends = p1 == pairs;
-        if (bad && lane == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_PAGE_ID);
-        if (begins && ends) {
-          const float inv = bad || l == 0.0f ? 0.0f : 1.0f / l;
-          if (col < G) {
+        if (lane == 0) s.seg[at] = cs.row * a.Hkv + cs.head;
+      }
+    };
+    auto attend = [&](Pair& b) __attribute__((always_inline)) {
+      v4f x[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+      for (int pg = 0; pg < 2; ++pg) x[pg] = q.scores(b.k[pg], b.ks[pg]);
+      const int left = cs.len - cp * 2 * P;
+      if (left < 2 * P) {  // tokens past the row's end: no weight, whatever the record holds there
+        asm volatile("");  // kept a branch: as selects in every pair it is a fifth of the arithmetic
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                h8v o;
+        for (int pg = 0; pg < 2; ++pg) {
+          const int n = min(max(left - pg * P - 4 * grp, 0), 4);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const float y = st.acc[4 * half + (e & 3)][2 * j + (e >> 2)] * inv;
-                  o[e] = (_Float16)(bad ? 0.0f : y);
-                }
-                *reinterpret_cast<h8v*>(out + col * D + half * 64 + grp * 16 + j * 8) = o;
-              }
+          for (int i = 0; i < 4; ++i) {
+            x[pg][i] = i < n ? x[pg][i] : -__builtin_inff();
+            b.vs[pg][i] = i < n ? b.vs[pg][i] : 0.0f;
           }
-        } else {
-          const int at = 2 * wave + (begins ? 1 : 0);
-          float* part = s.part + at * slot;
-          if (col < G) {
+          const unsigned keep = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<v4f*>(part + col * D + half * 64 + grp * 16 + i * 4) =
-                    v4f{st.acc[4 * half][i], st.acc[4 * half + 1][i], st.acc[4 * half + 2][i], st.acc[4 * half + 3][i]};
-            if (grp == 0) {
-              part[G * D + 2 * col] = st.m;
-              part[G * D + 2 * col + 1] = bad ? -1.0f : l;
-            }
-          }
-          if (lane == 0) s.seg[at] = row * a.Hkv + head;
+          for (int h = 0; h < 2; ++h) b.v[pg][h] &= v4u{keep, keep, keep, keep};
         }
       }
-      // ---- on to the next segment
-      u += n_units;
-      off = 0;
-      if (++head == a.Hkv) {
-        head = 0;
-        ++row;
-        if (u < u_end) c_units = uniform(s.pre[row + 1] - s.pre[row]);
+      float top = m;
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, x[pg][i]);
+      top = across_rows(top, [](float y, float z) { return fmaxf(y, z); });
+      if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
+        const float c = ex2(m - top);
+        l *= c;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[t] *= v4f{c, c, c, c};
+        m = top;
       }
+      b8v w;
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = ex2(x[pg][i] - m);
+          l += e;
+          const float f = e * b.vs[pg][i];
+          const __bf16 hi = (__bf16)f;
+          w[4 * pg + i] = col < 8 ? hi : (__bf16)(f - (float)hi);
+        }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<F>(b.v[0][t >> 2][t & 3], b.v[1][t >> 2][t & 3]), w, acc[t], 0, 0, 0);
+        if (t & 1) __builtin_amdgcn_sched_barrier(0);  // the conversions of a few tiles at a time: else they spill
+      }
+      ++cp;
+    };
+
+    // ---- the stream: a pair is computed while the next one loads
+    Pair b0, b1;
+    bool more = enter_segment(), in0 = false, in1 = false;
+    if (more) {
+      load_pair(b0);
+      in0 = true;
+      if (lp < ls.p1) {
+        load_pair(b1);
+        in1 = true;
+      }
+      begin_segment();
+      if (!in1) in1 = load(b1);
+    }
+    auto step = [&](Pair& b, bool& in) __attribute__((always_inline)) {
+      attend(b);
+      if (cp == cs.p1) {
+        end_segment();
+        if (ahead) begin_segment();
+      }
+      in = load(b);
+    };
+    while (in0) {
+      step(b0, in0);
+      if (!in1) break;
+      step(b1, in1);
     }
   }
   __syncthreads();

@@ -209,6 +209,7 @@ template <typename V>
 inline float __builtin_amdgcn_fdot2(V a, V b, float c, bool) { return std::fma((float)a[1], (float)b[1], std::fma((float)a[0], (float)b[0], c)); }
 inline float __builtin_amdgcn_exp2f(float x) { return std::exp2(x); }
 inline void __builtin_amdgcn_s_waitcnt(int) {}
+inline void __builtin_amdgcn_sched_barrier(int) {}
 inline void __builtin_amdgcn_s_sleep(int) { emu::yield(); }
 inline void __builtin_amdgcn_wave_barrier() { emu::wave_sync("wave_barrier"); }
 #define __builtin_amdgcn_fence(...) (void)0
@@ -301,6 +302,20 @@ inline unsigned to_e4m3(float x) {  // nearest, ties to even; beyond the largest
   return best | (std::signbit(x) ? 128 : 0);
 }
 }  // namespace emu
+// int8, 16 values of k a lane; sums in int32 (exact).
+namespace emu {
+typedef int i4 __attribute__((ext_vector_type(4)));
+template <typename V>
+inline i4 mfma_i8_k64(V a, V b, i4 c) {
+  const Operands* o = operands(&a, &b, 16, "mfma");
+  const int grp = lane() >> 4, col = lane() & 15;
+  for (int r = 0; r < 4; ++r)
+    for (int k = 0; k < 64; ++k)
+      c[r] += (int)(signed char)o->a[(k / 16) * 16 + 4 * grp + r][k % 16] * (int)(signed char)o->b[(k / 16) * 16 + col][k % 16];
+  return c;
+}
+}  // namespace emu
+#define __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, ...) (emu::wave_sync("mfma operands"), emu::mfma_i8_k64(a, b, c))
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, ...) (emu::wave_sync("mfma operands"), emu::mfma_bf16_k32(a, b, c))
 inline unsigned __builtin_amdgcn_perm(unsigned hi, unsigned lo, unsigned sel) {
   const uint64_t all = (uint64_t)hi << 32 | lo;
