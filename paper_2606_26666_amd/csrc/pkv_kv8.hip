@@ -54,14 +54,23 @@ __device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
 }
 
 // ---------------------------------------------------------------------------------
-// Formats. `load8` makes the bf16 operand of eight codes (exact: int8 has 8 and e4m3 4 significant
-// bits); `code` rounds x * top / m, where the product is exact in fp32 (11 + 7 bits) and the
-// division correctly rounded: a quotient of such numbers that is not on a rounding border is at
-// least 2^-19 of its size away from it, so the code is that of real arithmetic.
+// Formats. `load4` makes bf16 operands of codes (exact: int8 has 8 and e4m3 4 significant bits).
+// `code4` rounds quotients t = x * top / m, x and m of 11 bits each. A t that is not on a rounding
+// border is 2^-19 of its size or more away from the nearest one, and a border has at most 9 bits. So
+// x * (top / m) in fp32, off by less than 2^-23, is first rounded to 21 bits (round21), which puts a
+// t on a border back on it and no other there: the code is that of real arithmetic, ties included,
+// with one division a vector instead of one a value.
+__device__ __forceinline__ float round21(float y) { return as_f32((as_u32(y) + 4u) & ~7u); }
+
 struct Int8 {
   static constexpr float top = 127.0f;
-  static __device__ __forceinline__ unsigned code(float y) { return (unsigned)(int)__builtin_rintf(y) & 255u; }
-  static __device__ __forceinline__ float value(unsigned c) { return (float)(signed char)c; }
+  // 1.5 * 2^23 + y rounds y to an integer (ties to even), which is then the low bits of the sum.
+  static __device__ __forceinline__ unsigned code4(float a, float b, float c, float d) {
+    const unsigned x = __builtin_amdgcn_perm(as_u32(b + 12582912.0f), as_u32(a + 12582912.0f), 0x0C0C0400u);
+    const unsigned y = __builtin_amdgcn_perm(as_u32(d + 12582912.0f), as_u32(c + 12582912.0f), 0x04000C0Cu);
+    return x | y;
+  }
+  static __device__ __forceinline__ float value(unsigned w, int at) { return (float)(signed char)(w >> (8 * at)); }
   // Four codes as bf16: fp32 integers of at most 8 bits, whose upper 16 bits are the bf16s.
   static __device__ __forceinline__ v2u load4(unsigned w) {
     asm volatile("" : "+v"(w));  // one register: the compiler would carry the masked codes in one each
@@ -128,10 +137,15 @@ struct Int8 {
 };
 struct E4m3 {
   static constexpr float top = 448.0f;
-  static __device__ __forceinline__ unsigned code(float y) {
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 255u;
+  static __device__ __forceinline__ unsigned code4(float a, float b, float c, float d) {
+    const int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
   }
-  static __device__ __forceinline__ float value(unsigned c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
+  static __device__ __forceinline__ float value(unsigned w, int at) {
+    return at == 0 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 0)
+                   : at == 1 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 1)
+                             : at == 2 ? __builtin_amdgcn_cvt_f32_fp8((int)w, 2) : __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+  }
   static __device__ __forceinline__ v2u load4(unsigned w) {
     return v2u{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
@@ -168,114 +182,218 @@ struct E4m3 {
 
 // ---------------------------------------------------------------------------------
 // Append and gather.
+//
+// Both are bound by their bytes (776 a token and KV head). A wave takes a window of four packed
+// tokens and a range of KV heads, sixteen lanes a token, eight values a lane: 256-byte rows of fp16
+// on one side, 128-byte rows of K codes on the other. V codes lie in groups of four tokens: where
+// the wave's four are such a group, a transpose between the four lane groups (two swaps) makes whole
+// dwords, eight bytes a lane; else single bytes. A window's tokens may start inside a group, so a wave
+// takes the groups that begin in its window: a group begins at its row's first token or at a
+// position that is a multiple of four. Calls of few tokens per row (kScatter: one token per row, or
+// fewer than four on average) take the window's tokens side by side instead, in bytes.
 
-// Where packed token t goes: its row (the last i with offsets[i] <= t) and position. False when the
-// token is not to be touched; `zero`: it is to be read back as zeros. Safe for any offsets.
+// The last i with offsets[i] <= t (0 if there is none), with the wave's 64 lanes at once. In range
+// for any offsets.
+__device__ __forceinline__ int row_of(const Kv8MoveArgs& a, int t, int lane) {
+  int lo = 0, n = a.B;
+  while (n > 1) {
+    const int step = (n + 63) >> 6;
+    const int i = lane * step;
+    const bool below = i < n && a.offsets[lo + i] <= t;
+    const int c = max(__popcll(__builtin_amdgcn_ballot_w64(below)) - 1, 0);
+    lo += c * step;
+    n = min(step, n - c * step);
+  }
+  return uniform(lo);
+}
+
+// A token's place. `there`: it is to be moved; `zero`: it is to be read back as zeros (both false:
+// it is left alone). `begin`, `end`: the row's packed tokens.
 struct Place {
-  int row, pos;
+  int row, pos, begin, end;
   bool there, zero;
 };
-__device__ __forceinline__ Place place(const Kv8MoveArgs& a, int t) {
-  Place p{t, 0, true, false};
-  int end = t + 1;
+__device__ __forceinline__ Place place(const Kv8MoveArgs& a, int t, int row) {
+  Place p{row, 0, t, t + 1, false, false};
   if (a.offsets) {
-    int lo = 0, hi = a.B;  // offsets[lo] <= t < offsets[hi], as far as they ascend
-    if (t >= a.offsets[a.B] || t < a.offsets[0]) return Place{0, 0, false, false};
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.offsets[mid] <= t) lo = mid; else hi = mid;
-    }
-    p.row = lo;
-    end = a.offsets[lo + 1];
+    p.begin = a.offsets[row];
+    p.end = a.offsets[row + 1];
+    if (t < p.begin || t >= a.offsets[a.B]) return p;
   }
-  const int len = a.seq_lens[p.row];
-  const int begin = a.offsets ? a.offsets[p.row] : t;
-  if (!a.offsets && len == 0) return Place{0, 0, false, true};
-  if (len < 0 || len > a.max_pages_per_row * P || begin < 0 || end < begin || end - begin > len) {
+  const int len = a.seq_lens[row];
+  p.zero = true;
+  if (!a.offsets && len == 0) return p;
+  // (p.begin <= t here) the row's tokens end after t and are no more than its length
+  if (len < 0 || len > a.max_pages_per_row * P || p.begin < 0 || p.end <= t || p.end - p.begin > len) {
     atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
-    return Place{0, 0, false, true};
+    return p;
   }
-  p.pos = len - (end - t);
+  p.there = true;
+  p.zero = false;
+  p.pos = len - (p.end - t);
   return p;
 }
 
-__device__ __forceinline__ uint8_t* record(const Kv8MoveArgs& a, Place& p, int h) {
-  const int id = a.block_table[(size_t)p.row * a.max_pages_per_row + p.pos / P];
-  if (id < 0 || id >= a.num_pages) {
-    atomicOr(a.err, (unsigned)PKV_DEVERR_PAGE_ID);
-    p.there = false;
-    p.zero = true;
-    return a.cache;
-  }
-  return a.cache + ((size_t)id * a.Hkv + h) * kKv8Record;
+// The page of a position as an offset of records; a bad id takes the token out.
+__device__ __forceinline__ size_t page_at(const Kv8MoveArgs& a, int row, int pos, bool& there, bool& zero) {
+  const int id = a.block_table[(size_t)row * a.max_pages_per_row + pos / P];
+  if (id >= 0 && id < a.num_pages) return (size_t)id * a.Hkv * kKv8Record;
+  atomicOr(a.err, (unsigned)PKV_DEVERR_PAGE_ID);
+  there = false;
+  zero = true;
+  return 0;
 }
 
-// Sixteen lanes per (token, KV head), eight values a lane.
+// Sixteen-bit units between the four 16-lane groups: lane group j gives its units 0 .. 3 (two dwords)
+// and receives unit j of groups 0 .. 3, as bytes: word i of the result holds byte i of the units.
+__device__ __forceinline__ v2u groups_to_words(v2u w) {
+  const auto r = __builtin_amdgcn_permlane32_swap(w.x, w.y, false, false);
+  const unsigned x = (unsigned)r[0], y = (unsigned)r[1];
+  const unsigned p = __builtin_amdgcn_perm(y, x, 0x05040100u), q = __builtin_amdgcn_perm(y, x, 0x07060302u);
+  const auto t = __builtin_amdgcn_permlane16_swap(p, q, false, false);
+  const unsigned even = (unsigned)t[0], odd = (unsigned)t[1];  // groups 0 and 2, groups 1 and 3
+  return v2u{__builtin_amdgcn_perm(odd, even, 0x06020400u), __builtin_amdgcn_perm(odd, even, 0x07030501u)};
+}
+// The way back.
+__device__ __forceinline__ v2u words_to_groups(v2u w) {
+  const unsigned even = __builtin_amdgcn_perm(w.y, w.x, 0x06020400u), odd = __builtin_amdgcn_perm(w.y, w.x, 0x07030501u);
+  const auto t = __builtin_amdgcn_permlane16_swap(even, odd, false, false);
+  const unsigned p = (unsigned)t[0], q = (unsigned)t[1];
+  const unsigned x = __builtin_amdgcn_perm(q, p, 0x05040100u), y = __builtin_amdgcn_perm(q, p, 0x07060302u);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  return v2u{(unsigned)r[0], (unsigned)r[1]};
+}
+
+__device__ __forceinline__ unsigned row_max16(unsigned m) {
+  m = max(m, (unsigned)dpp<0xB1>((int)m));
+  m = max(m, (unsigned)dpp<0x4E>((int)m));
+  m = max(m, (unsigned)dpp<0x141>((int)m));
+  return max(m, (unsigned)dpp<0x140>((int)m));
+}
+
+// Eight values a lane, sixteen lanes a vector, to codes and the vector's scale.
 template <typename F>
-__global__ __launch_bounds__(256) void append_kernel(Kv8MoveArgs a) {
-  const int c = threadIdx.x & 15;
-  const long long n = (long long)a.tokens * a.Hkv;
-  for (long long i = (blockIdx.x * 256ll + threadIdx.x) >> 4; i < n; i += gridDim.x * 16ll) {
-    const int t = (int)(i / a.Hkv), h = (int)(i % a.Hkv);
-    Place p = place(a, t);
-    if (!p.there) continue;
-    uint8_t* rec = record(a, p, h);
-    if (!p.there) continue;
-    const int s = p.pos % P;
+__device__ __forceinline__ v2u quantise(v4u raw, float& scale) {
+  unsigned m = 0;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const uint16_t* src = kv ? a.v + (size_t)t * a.v_stride : a.k + (size_t)t * a.k_stride;
-      const v4u raw = *reinterpret_cast<const v4u*>(src + (size_t)h * D + c * 8);
-      unsigned m = 0;
+  for (int j = 0; j < 4; ++j) m = max(m, max(raw[j] & 0x7FFFu, (raw[j] >> 16) & 0x7FFFu));
+  m = row_max16(m);
+  const bool finite = m < 0x7C00u;
+  const float top = (float)__builtin_bit_cast(_Float16, (uint16_t)m);
+  const float inv = finite && m > 0 ? F::top / top : 0.0f;
+  scale = finite ? top / F::top : as_f32(0x7FC00000u);
+  const h8v x = __builtin_bit_cast(h8v, raw);
+  float y[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m = max(m, raw[j] & 0x7FFFu);
-        m = max(m, (raw[j] >> 16) & 0x7FFFu);
-      }
-#pragma unroll
-      for (int x = 1; x < 16; x <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, x));
-      const bool finite = m < 0x7C00u;
-      const float top = (float)__builtin_bit_cast(_Float16, (uint16_t)m);
-      const h8v x = __builtin_bit_cast(h8v, raw);
-      uint8_t code[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) code[j] = finite && m > 0 ? (uint8_t)F::code((float)x[j] * F::top / top) : 0;
-      if (kv == 0) {
-        *reinterpret_cast<v2u*>(rec + s * D + c * 8) = __builtin_bit_cast(v2u, code);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) rec[kKv8CodeBytes + (s / 4) * (4 * D) + (c * 8 + j) * 4 + s % 4] = code[j];
-      }
-      if (c == 0) reinterpret_cast<float*>(rec + kKv8ScaleAt)[kv * P + s] = finite ? top / F::top : as_f32(0x7FC00000u);
+  for (int j = 0; j < 8; ++j) y[j] = finite ? round21((float)x[j] * inv) : 0.0f;
+  return v2u{F::code4(y[0], y[1], y[2], y[3]), F::code4(y[4], y[5], y[6], y[7])};
+}
+
+struct Append {
+  // One KV head of the window: `there` per 16 lanes; `group`: all four are one group of the record.
+  template <typename F>
+  static __device__ __forceinline__ void head(const Kv8MoveArgs& a, int t, bool there, bool, size_t rec_at, int s, int h, int grp,
+                                              int c, bool group) {
+    uint8_t* rec = a.cache + rec_at + (size_t)h * kKv8Record;
+    v4u raw[2] = {};
+    if (there) {
+      raw[0] = *reinterpret_cast<const v4u*>(a.k + (size_t)t * a.k_stride + h * D + c * 8);
+      raw[1] = *reinterpret_cast<const v4u*>(a.v + (size_t)t * a.v_stride + h * D + c * 8);
     }
+    float scale[2];
+    const v2u kc = quantise<F>(raw[0], scale[0]);
+    v2u vc = quantise<F>(raw[1], scale[1]);
+    uint8_t* v = rec + kKv8CodeBytes + (s / 4) * (4 * D);
+    if (group) {
+      vc = groups_to_words(vc);
+      *reinterpret_cast<v2u*>(v + (c * 8 + 2 * grp) * 4) = vc;
+    }
+    if (!there) return;
+    *reinterpret_cast<v2u*>(rec + s * D + c * 8) = kc;
+    if (!group) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[(c * 8 + j) * 4 + s % 4] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
+    }
+    if (c < 2) reinterpret_cast<float*>(rec + kKv8ScaleAt)[c * P + s] = c ? scale[1] : scale[0];
   }
-}
+};
 
-template <typename F>
-__global__ __launch_bounds__(256) void gather_kernel(Kv8MoveArgs a) {
-  const int c = threadIdx.x & 15;
-  const long long n = (long long)a.tokens * a.Hkv;
-  for (long long i = (blockIdx.x * 256ll + threadIdx.x) >> 4; i < n; i += gridDim.x * 16ll) {
-    const int t = (int)(i / a.Hkv), h = (int)(i % a.Hkv);
-    Place p = place(a, t);
-    const uint8_t* rec = a.cache;
-    if (p.there) rec = record(a, p, h);
-    if (!p.there && !p.zero) continue;
-    const int s = p.pos % P;
+struct Gather {
+  template <typename F>
+  static __device__ __forceinline__ void head(const Kv8MoveArgs& a, int t, bool there, bool zero, size_t rec_at, int s, int h, int grp,
+                                              int c, bool group) {
+    const uint8_t* rec = a.cache + rec_at + (size_t)h * kKv8Record;
+    const uint8_t* v = rec + kKv8CodeBytes + (s / 4) * (4 * D);
+    v2u kc = {}, vc = {};
+    float ks = 0.0f, vs = 0.0f;
+    if (there) {
+      kc = *reinterpret_cast<const v2u*>(rec + s * D + c * 8);
+      ks = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[s];
+      vs = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[P + s];
+    }
+    if (group) {
+      vc = words_to_groups(*reinterpret_cast<const v2u*>(v + (c * 8 + 2 * grp) * 4));
+    } else if (there) {
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      h8v x = {};
-      if (p.there) {
-        const float scale = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[kv * P + s];
+      for (int j = 0; j < 8; ++j) vc[j >> 2] |= (unsigned)v[(c * 8 + j) * 4 + s % 4] << (8 * (j & 3));
+    }
+    if (!there && !zero) return;
+    h8v x, y;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint8_t code = kv == 0 ? rec[s * D + c * 8 + j]
-                                       : rec[kKv8CodeBytes + (s / 4) * (4 * D) + (c * 8 + j) * 4 + s % 4];
-          x[j] = (_Float16)(F::value(code) * scale);
+    for (int j = 0; j < 8; ++j) {
+      x[j] = (_Float16)(F::value(kc[j >> 2], j & 3) * ks);
+      y[j] = (_Float16)(F::value(vc[j >> 2], j & 3) * vs);
+    }
+    *reinterpret_cast<h8v*>(a.k + (size_t)t * a.k_stride + h * D + c * 8) = x;
+    *reinterpret_cast<h8v*>(a.v + (size_t)t * a.v_stride + h * D + c * 8) = y;
+  }
+};
+
+constexpr int kMoveWaves = 4;  // of a workgroup
+
+template <typename Op, typename F, bool kScatter>
+__global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, int chunks, int chunk) {
+  const int lane = threadIdx.x & 63, grp = lane >> 4, c = lane & 15;
+  const long long units = ((long long)a.tokens + 3) / 4 * chunks;
+  for (long long unit = (long long)blockIdx.x * kMoveWaves + uniform(threadIdx.x >> 6); unit < units;
+       unit += (long long)gridDim.x * kMoveWaves) {
+    const int w0 = (int)(unit / chunks) * 4, h0 = (int)(unit % chunks) * chunk, h1 = min(h0 + chunk, a.Hkv);
+    auto heads = [&](int t, bool there, bool zero, size_t rec, int s, bool group) __attribute__((always_inline)) {
+      for (int h = h0; h < h1; ++h) Op::template head<F>(a, t, there, zero, rec, s, h, grp, c, group);
+    };
+    const int left = a.tokens - w0;
+    if (kScatter) {
+      const int t = w0 + min(grp, left - 1);
+      int row = min(t, a.B - 1);
+      if (a.offsets) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = row_of(a, w0 + min(j, left - 1), lane);
+          if (grp == j) row = r;
         }
       }
-      uint16_t* dst = kv ? a.v + (size_t)t * a.v_stride : a.k + (size_t)t * a.k_stride;
-      *reinterpret_cast<h8v*>(dst + (size_t)h * D + c * 8) = x;
+      Place p = place(a, t, row);
+      size_t rec = 0;
+      if (p.there) rec = page_at(a, p.row, p.pos, p.there, p.zero);
+      heads(t, p.there && grp < left, p.zero && grp < left, rec, p.pos % P, false);
+      continue;
+    }
+    const int w1 = left < 4 ? a.tokens : w0 + 4;
+    for (int t = w0; t < w1;) {
+      const Place p = place(a, t, row_of(a, t, lane));
+      if (!p.there) {  // left alone, or zeros, a token at a time
+        if (p.zero) heads(t, false, grp == 0, 0, 0, false);
+        ++t;
+        continue;
+      }
+      const int first = p.pos & 3;
+      const int n = min(min(p.end, a.tokens) - t, 4 - first);
+      if (t == p.begin || first == 0) {
+        bool there = grp >= first && grp < first + n, zero = false, page = true;
+        const size_t rec = page_at(a, p.row, p.pos, page, zero);
+        heads(t + grp - first, there && page, there && !page, rec, (p.pos & ~3) % P + grp, n == 4 && page);
+      }
+      t += n;
     }
   }
 }
@@ -787,22 +905,33 @@ hipError_t launch_kv8_decode(const Kv8DecodeArgs& a, int format, hipStream_t s) 
 }
 
 namespace {
-unsigned move_grid(const Kv8MoveArgs& a) {
-  const long long blocks = ((long long)a.tokens * a.Hkv + 15) / 16;
-  return (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+
+// Heads per wave: one, as long as the waves then are no more than the device can hold some eight
+// times over, so that small calls spread; beyond, several, which share the lookups.
+constexpr long long kMoveUnits = 65536;
+
+template <typename Op, typename F>
+hipError_t launch_move(const Kv8MoveArgs& a, hipStream_t s) {
+  const long long windows = ((long long)a.tokens + 3) / 4;
+  long long chunk = (windows * a.Hkv + kMoveUnits - 1) / kMoveUnits;
+  if (chunk > a.Hkv) chunk = a.Hkv;
+  const long long chunks = (a.Hkv + chunk - 1) / chunk;
+  long long blocks = (windows * chunks + kMoveWaves - 1) / kMoveWaves;
+  if (blocks > 1 << 22) blocks = 1 << 22;  // a launch's size in threads has 32 bits
+  const bool scatter = !a.offsets || a.tokens < 4ll * a.B;
+  if (scatter) hipLaunchKernelGGL((move_kernel<Op, F, true>), dim3((unsigned)blocks), dim3(kMoveWaves * 64), 0, s, a, (int)chunks, (int)chunk);
+  else hipLaunchKernelGGL((move_kernel<Op, F, false>), dim3((unsigned)blocks), dim3(kMoveWaves * 64), 0, s, a, (int)chunks, (int)chunk);
+  return hipGetLastError();
 }
+
 }  // namespace
 
 hipError_t launch_kv8_append(const Kv8MoveArgs& a, int format, hipStream_t s) {
-  if (format == PKV_KV8_INT8) hipLaunchKernelGGL(append_kernel<Int8>, dim3(move_grid(a)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(append_kernel<E4m3>, dim3(move_grid(a)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return format == PKV_KV8_INT8 ? launch_move<Append, Int8>(a, s) : launch_move<Append, E4m3>(a, s);
 }
 
 hipError_t launch_kv8_gather(const Kv8MoveArgs& a, int format, hipStream_t s) {
-  if (format == PKV_KV8_INT8) hipLaunchKernelGGL(gather_kernel<Int8>, dim3(move_grid(a)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(gather_kernel<E4m3>, dim3(move_grid(a)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return format == PKV_KV8_INT8 ? launch_move<Gather, Int8>(a, s) : launch_move<Gather, E4m3>(a, s);
 }
 
 }  // namespace pkv

@@ -112,7 +112,7 @@ template <typename K, typename... A>
 inline void emu_launch(K kernel, dim3 grid, dim3 block, A... args) {
   emu::run((const void*)kernel, grid, block, [&] { kernel(args...); });
 }
-#define hipLaunchKernelGGL(kernel, grid, block, shared, stream, ...) emu_launch(kernel, grid, block, __VA_ARGS__)
+#define hipLaunchKernelGGL(kernel, grid, block, shared, stream, ...) emu_launch((kernel), grid, block, __VA_ARGS__)
 #define hipExtLaunchKernelGGL(kernel, grid, block, shared, stream, start, stop, flags, ...) \
   emu_launch(kernel, grid, block, __VA_ARGS__)
 
@@ -320,7 +320,11 @@ inline i4 mfma_i8_k64(V a, V b, i4 c) {
 inline unsigned __builtin_amdgcn_perm(unsigned hi, unsigned lo, unsigned sel) {
   const uint64_t all = (uint64_t)hi << 32 | lo;
   unsigned r = 0;
-  for (int i = 0; i < 4; ++i) r |= (unsigned)(all >> (8 * ((sel >> (8 * i)) & 7)) & 255) << (8 * i);
+  for (int i = 0; i < 4; ++i) {  // selector 12: zero
+    const unsigned at = sel >> (8 * i) & 255;
+    if (at > 7 && at != 12) emu::fail("perm selector");
+    if (at < 8) r |= (unsigned)(all >> (8 * at) & 255) << (8 * i);
+  }
   return r;
 }
 inline int __builtin_amdgcn_cvt_pk_fp8_f32(float a, float b, int old, bool high) {
