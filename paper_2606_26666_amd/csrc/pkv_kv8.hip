@@ -19,6 +19,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 
+constexpr int kNt = 2;    // cache-policy operand of a buffer access: non-temporal (a call reads each record once)
+constexpr int kOutOfRange = (int)0x80000000u;  // an offset past any buffer: reads as zero, without memory
 constexpr int kSc1 = 16;  // cache-policy operand of a buffer access: coherent across the XCDs' L2 caches
 constexpr float kLowest = -3.0e38f;  // a finite start for running maxima: no infinity is subtracted from another
 
@@ -51,6 +53,16 @@ template <typename F>
 __device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
   const v2u a = F::load4(lo), b = F::load4(hi);
   return __builtin_bit_cast(b8v, v4u{a.x, a.y, b.x, b.y});
+}
+
+// All 64 lanes combined, in a fixed order.
+template <typename F>
+__device__ __forceinline__ float across_wave(float x, F f) {
+  x = f(x, as_f32((unsigned)dpp<0xB1>((int)as_u32(x))));
+  x = f(x, as_f32((unsigned)dpp<0x4E>((int)as_u32(x))));
+  x = f(x, as_f32((unsigned)dpp<0x141>((int)as_u32(x))));
+  x = f(x, as_f32((unsigned)dpp<0x140>((int)as_u32(x))));
+  return across_rows(x, f);
 }
 
 // ---------------------------------------------------------------------------------
@@ -427,17 +439,35 @@ struct Pair {
   v4f ks[2], vs[2];
 };
 
+// The partial states of a segment in a workgroup: entries at .. at + n - 1 of Lds::seg, those of
+// them that `valid` has.
+struct Group {
+  int seg, at, n;
+  unsigned valid;
+  int first, last;  // workgroups with states of the segment
+};
+
 struct Lds {
   int pre[kMaxPlanBatch + 1];  // units before each row, for one KV head
   int len[kMaxPlanBatch];
   int wave_sum[W];
   int seg[2 * W];    // segment of each wave's partial states (-1: none): one it continues, one it begins
-  int group_at[2 * W], group_n[2 * W];
+  Group group[2 * W];
   int groups, last[2];
+  float head_l[kKv8MaxG];
   __align__(16) float part[2 * W * (kKv8MaxG * D + 2 * kKv8MaxG)];
 };
 
 __device__ __forceinline__ int pairs_of(int len) { return (int)(((unsigned)len + 2 * P - 1) / (2 * P)); }
+
+// Four values of an output from their sums, the sum of weights and whether the row is zeroed.
+__device__ __forceinline__ void store_out(uint16_t* out, v4f A, float L, bool zero) {
+  const float inv = zero || L == 0.0f ? 0.0f : 1.0f / L;
+  uint16_t o[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = zero ? 0 : __builtin_bit_cast(uint16_t, (_Float16)(A[e] * inv));
+  *reinterpret_cast<v2u*>(out) = __builtin_bit_cast(v2u, o);
+}
 
 // The part of a segment that a wave has: pairs p0 .. p1 - 1 of `pairs`.
 struct Segment {
@@ -538,13 +568,17 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       return false;
     };
 
-    // ---- the load cursor: at most one segment ahead of the one being computed
+    // ---- the load cursor: pairs go into two buffers, those at an even distance from the start of
+    // the wave's part of a segment into the first. A pair that there is not loads through an empty
+    // descriptor, which reads nothing: with the same loads on every path the compiler waits for a
+    // buffer's own loads only, not for all that may be under way.
     Segment ls, cs;
-    int lp = 0;             // next pair of ls to load
+    int lp = 0;                            // next pair of ls to load
     int ids = 0, ids_next = 0, ids_p = 0;  // ids of ls's pairs ids_p ..
     int tag_row = -1, tag_p = 0;           // what ids_next holds
     bool bad = false, bad_before = false;  // a bad page in ls; in cs when ls is ahead of it
-    bool ahead = false;                    // ls is not cs
+    bool ahead = false;                    // ls is the segment after cs
+    ls.p1 = 0;
     v4u qraw[4];
     const int myhead = col < 8 ? col : 15 - col;
     auto fetch_ids = [&](int r, int p) {
@@ -555,6 +589,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     auto enter_ids = [&](int p) __attribute__((always_inline)) {
       if (tag_row != ls.row || tag_p != p) ids_next = fetch_ids(ls.row, p);
       ids = ids_next;
+      asm volatile("" : "+v"(ids));  // waited for here, not where each pair reads it
       ids_p = p;
       // what comes next: this segment's next pairs, or the next segment's first (of the next row, if
       // that is not an empty one)
@@ -562,55 +597,49 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       else if (u < u_end) ids_next = fetch_ids(row, 0);
     };
     auto enter_segment = [&]() __attribute__((always_inline)) {
-      if (!next_segment(ls)) return false;
+      if (!next_segment(ls)) {
+        ls.p1 = lp = 0;
+        return;
+      }
+      ahead = true;
       lp = ls.p0;
+      bad_before = bad;
       bad = false;
       const uint16_t* q = a.q + (size_t)ls.row * a.q_stride + ((size_t)ls.head * G + (myhead < G ? myhead : 0)) * D + grp * 16;
 #pragma unroll
       for (int j = 0; j < 4; ++j) qraw[j] = *reinterpret_cast<const v4u*>(q + (j >> 1) * 64 + (j & 1) * 8);
       enter_ids(lp);
-      return true;
     };
-    auto load_pair = [&](Pair& b) __attribute__((always_inline)) {
-      if (lp - ids_p == kIdPairs) enter_ids(lp);
-      const int pages = (ls.len + P - 1) / P;
+    const int k_at = col * D + grp * 16, v_at = kKv8CodeBytes + grp * (4 * D) + col * 16, s_at = kKv8ScaleAt + grp * 16;
+    auto load = [&](Pair& b) __attribute__((always_inline)) {
+      const bool there = lp < ls.p1;
+      const int left = there ? ls.len - lp * 2 * P : 0;  // tokens from the pair on
+      if (there && lp - ids_p == kIdPairs) enter_ids(lp);
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
-        int id = __builtin_amdgcn_readlane(ids, 2 * (lp - ids_p) + (2 * lp + pg < pages ? pg : 0));
-        if (id < 0 || id >= a.num_pages) {
-          bad = true;
-          id = 0;
-        }
-        const uint8_t* rec = a.cache + ((size_t)id * a.Hkv + ls.head) * kKv8Record;
-        const v4u* kp = reinterpret_cast<const v4u*>(rec + col * D + grp * 16);
-        const v4u* vp = reinterpret_cast<const v4u*>(rec + kKv8CodeBytes + grp * (4 * D) + col * 16);
-        const v4f* sp = reinterpret_cast<const v4f*>(rec + kKv8ScaleAt + grp * 16);
-        b.k[pg][0] = __builtin_nontemporal_load(kp);
-        b.k[pg][1] = __builtin_nontemporal_load(kp + 4);
-        b.ks[pg] = __builtin_nontemporal_load(sp);
-        b.v[pg][0] = __builtin_nontemporal_load(vp);
-        b.v[pg][1] = __builtin_nontemporal_load(vp + 16);
-        b.vs[pg] = __builtin_nontemporal_load(sp + 4);
+        int id = there ? __builtin_amdgcn_readlane(ids, (2 * (lp - ids_p) + pg) & 63) : 0;
+        const bool page = left > pg * P;
+        const bool good = id >= 0 && id < a.num_pages;
+        if (page && !good) bad = true;
+        id = page && good ? id : 0;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t*>(a.cache + ((size_t)id * a.Hkv + (there ? ls.head : 0)) * kKv8Record), (short)0,
+            page && good ? kKv8Record : 0, 0x00020000);
+        b.k[pg][0] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at, 0, kNt);
+        b.k[pg][1] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at + 64, 0, kNt);
+        b.ks[pg] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, s_at, 0, kNt));
+        b.v[pg][0] = __builtin_amdgcn_raw_buffer_load_b128(r, v_at, 0, kNt);
+        b.v[pg][1] = __builtin_amdgcn_raw_buffer_load_b128(r, v_at + 256, 0, kNt);
+        b.vs[pg] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, s_at + 64, 0, kNt));
       }
-      ++lp;
-    };
-    // Whether a pair was left to load.
-    auto load = [&](Pair& b) __attribute__((always_inline)) {
-      if (lp == ls.p1) {
-        const bool before = bad;
-        if (!enter_segment()) return false;
-        bad_before = before;
-        ahead = true;
-      }
-      load_pair(b);
-      return true;
+      lp += there;
     };
 
     // ---- the segment being computed
     typename F::Query q;
     v4f acc[8];  // tile t, row 4 grp + i: dim 16 grp + 4 i + t (t < 4) or 64 + 16 grp + 4 i + t - 4
     float m, l;
-    int cp;
+    int cp = 0;
     auto begin_segment = [&]() __attribute__((always_inline)) {
       cs = ls;
       ahead = false;
@@ -662,11 +691,11 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
         if (lane == 0) s.seg[at] = cs.row * a.Hkv + cs.head;
       }
     };
-    auto attend = [&](Pair& b) __attribute__((always_inline)) {
+    auto attend = [&](Pair& b, int pair) __attribute__((always_inline)) {
       v4f x[2];
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) x[pg] = q.scores(b.k[pg], b.ks[pg]);
-      const int left = cs.len - cp * 2 * P;
+      const int left = cs.len - pair * 2 * P;
       if (left < 2 * P) {  // tokens past the row's end: no weight, whatever the record holds there
         asm volatile("");  // kept a branch: as selects in every pair it is a fifth of the arithmetic
 #pragma unroll
@@ -711,102 +740,83 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
         acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<F>(b.v[0][t >> 2][t & 3], b.v[1][t >> 2][t & 3]), w, acc[t], 0, 0, 0);
         if (t & 1) __builtin_amdgcn_sched_barrier(0);  // the conversions of a few tiles at a time: else they spill
       }
-      ++cp;
     };
 
-    // ---- the stream: a pair is computed while the next one loads
+    // ---- the stream: two pairs are computed, each one's buffer then loads the pair after the other's
     Pair b0, b1;
-    bool more = enter_segment(), in0 = false, in1 = false;
-    if (more) {
-      load_pair(b0);
-      in0 = true;
-      if (lp < ls.p1) {
-        load_pair(b1);
-        in1 = true;
-      }
-      begin_segment();
-      if (!in1) in1 = load(b1);
-    }
-    auto step = [&](Pair& b, bool& in) __attribute__((always_inline)) {
-      attend(b);
-      if (cp == cs.p1) {
+    for (bool live = false;;) {
+      if (live) attend(b0, cp);
+      if (lp >= ls.p1) enter_segment();
+      load(b0);
+      if (live && cp + 1 < cs.p1) attend(b1, cp + 1);
+      load(b1);
+      if (live) {
+        cp += 2;
+        if (cp < cs.p1) continue;
         end_segment();
-        if (ahead) begin_segment();
       }
-      in = load(b);
-    };
-    while (in0) {
-      step(b0, in0);
-      if (!in1) break;
-      step(b1, in1);
+      if (!ahead) break;
+      begin_segment();
+      live = true;
     }
   }
   __syncthreads();
 
   // ---- states of segments that several waves share: runs of equal entries of s.seg
+  const int SB = slot * (int)sizeof(float);
   if (wave == 0) {
     const int mine = lane < 2 * W ? s.seg[lane] : -1;
     const unsigned long long valid = __builtin_amdgcn_ballot_w64(mine >= 0);
     const unsigned long long below = valid & ((1ull << lane) - 1);
     const int prev = __shfl(mine, below ? 63 - __builtin_clzll(below) : 0);
     const unsigned long long starts = __builtin_amdgcn_ballot_w64(mine >= 0 && (!below || prev != mine));
-    const int g = __popcll(starts & ((1ull << lane) - 1));
     if (starts >> lane & 1) {
-      s.group_at[g] = lane;
-      const unsigned long long next = lane < 63 ? starts >> (lane + 1) << (lane + 1) : 0;
-      s.group_n[g] = (next ? __builtin_ctzll(next) : 2 * W) - lane;
+      Group& g = s.group[__popcll(starts & ((1ull << lane) - 1))];
+      const unsigned long long next = starts & ~((2ull << lane) - 1);
+      g.seg = mine;
+      g.at = lane;
+      g.n = (next ? __builtin_ctzll(next) : 2 * W) - lane;
+      g.valid = (unsigned)(valid >> lane) & ((1u << g.n) - 1);
+      // the workgroups that hold states of the segment: those of its first to its last pair
+      const int r = mine / a.Hkv, h = mine - r * a.Hkv;
+      const int c = s.pre[r + 1] - s.pre[r], base = s.pre[r] * a.Hkv + h * c;
+      g.first = wave_of(base) / W;
+      g.last = wave_of(base + c - kSegment - 1) / W;
     }
     if (lane == 0) {
       s.groups = __popcll(starts);
-      s.last[0] = s.last[1] = 0;
+      s.last[0] = s.last[1] = -1;
     }
   }
   __syncthreads();
   const int cols = G * (D / 4);  // float4 columns of a state
-  const int SB = slot * (int)sizeof(float);
   const __amdgpu_buffer_rsrc_t pr =
       __builtin_amdgcn_make_buffer_rsrc(a.partials, (short)0, 2 * kKv8MaxWorkgroups * SB, 0x00020000);
-  // The workgroups that hold states of a segment: those of its first and its last pair.
-  auto span = [&](int seg, int& first, int& last) {
-    const int r = seg / a.Hkv, h = seg - r * a.Hkv;
-    const int c = s.pre[r + 1] - s.pre[r];
-    const int base = s.pre[r] * a.Hkv + h * c;
-    first = wave_of(base) / W;
-    last = wave_of(base + c - kSegment - 1) / W;
-  };
   const int groups = uniform(s.groups);
   for (int it = tid; it < groups * cols; it += W * 64) {
-    const int g = it / cols, e4 = it - g * cols, h = e4 / (D / 4);
-    const int at = s.group_at[g], n = s.group_n[g];
-    const int seg = s.seg[at];
-    int first, last;
-    span(seg, first, last);
+    const int gi = it / cols, e4 = it - gi * cols, h = e4 / (D / 4);
+    const Group g = s.group[gi];
+    const float* part = s.part + g.at * slot;
     float M = kLowest, L = 0.0f;
     bool zero = false;
-    for (int j = at; j < at + n; ++j) {
-      if (s.seg[j] != seg) continue;
-      const float* part = s.part + j * slot;
-      M = fmaxf(M, part[G * D + 2 * h]);
-      zero |= part[G * D + 2 * h + 1] < 0.0f;
+    for (int j = 0; j < g.n; ++j) {
+      if (!(g.valid >> j & 1)) continue;
+      M = fmaxf(M, part[j * slot + G * D + 2 * h]);
+      zero |= part[j * slot + G * D + 2 * h + 1] < 0.0f;
     }
     v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = at; j < at + n; ++j) {
-      if (s.seg[j] != seg) continue;
-      const float* part = s.part + j * slot;
-      const float c = ex2(part[G * D + 2 * h] - M);
-      const v4f x = *reinterpret_cast<const v4f*>(part + 4 * e4);
-      L = __builtin_fmaf(c, part[G * D + 2 * h + 1], L);
+    for (int j = 0; j < g.n; ++j) {
+      if (!(g.valid >> j & 1)) continue;
+      const float c = ex2(part[j * slot + G * D + 2 * h] - M);
+      const v4f x = *reinterpret_cast<const v4f*>(part + j * slot + 4 * e4);
+      L = __builtin_fmaf(c, part[j * slot + G * D + 2 * h + 1], L);
 #pragma unroll
       for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[e], A[e]);
     }
-    if (first == last) {
-      const float inv = zero || L == 0.0f ? 0.0f : 1.0f / L;
-      uint16_t o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = zero ? 0 : __builtin_bit_cast(uint16_t, (_Float16)(A[e] * inv));
-      *reinterpret_cast<v2u*>(a.out + (size_t)seg * G * D + 4 * e4) = __builtin_bit_cast(v2u, o);
+    if (g.first == g.last) {
+      store_out(a.out + (size_t)g.seg * G * D + 4 * e4, A, L, zero);
     } else {
-      const int so = (2 * blockIdx.x + (first == (int)blockIdx.x ? 1 : 0)) * SB;
+      const int so = (2 * blockIdx.x + (g.first == (int)blockIdx.x ? 1 : 0)) * SB;
       __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, A), pr, so + e4 * 16, 0, kSc1);
       if (e4 % (D / 4) == 0)
         __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
@@ -817,62 +827,83 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (tid < groups) {
-    const int seg = s.seg[s.group_at[tid]];
-    int first, last;
-    span(seg, first, last);
-    if (first != last) {
-      const int prev = __hip_atomic_fetch_add(&a.counters[seg], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (prev == last - first) {
+    const Group g = s.group[tid];
+    if (g.first != g.last) {
+      const int prev = __hip_atomic_fetch_add(&a.counters[g.seg], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (prev == g.last - g.first) {
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        s.last[first == (int)blockIdx.x ? 1 : 0] = seg + 1;
-        a.counters[seg] = 0;
+        s.last[g.first == (int)blockIdx.x ? 1 : 0] = tid;
+        a.counters[g.seg] = 0;
       }
     }
   }
   __syncthreads();
 
+  // ---- merge of a segment whose last state this workgroup brought. Threads take float4 columns,
+  // 16 / G of them a column, which share the states in turn; wave h makes the weights of head h.
   for (int which = 0; which < 2; ++which) {
-    const int seg = uniform(s.last[which]) - 1;
-    if (seg < 0) continue;
-    int first, last;
-    span(seg, first, last);
-    const int n = last - first + 1;
-    auto slot_at = [&](int j) { return (2 * (first + j) + (j == 0 ? 1 : 0)) * SB; };
-    float* wm = s.part;                          // [n][G] maxima, then weights
-    float* wl = wm + kKv8MaxWorkgroups * kKv8MaxG;  // [n][G] sums
-    for (int i = tid; i < n * G; i += W * 64) {
-      const int j = i / G, h = i - j * G;
-      const v2u ml = __builtin_amdgcn_raw_buffer_load_b64(pr, slot_at(j) + (G * D + 2 * h) * 4, 0, kSc1);
-      wm[i] = as_f32(ml.x);
-      wl[i] = as_f32(ml.y);
+    const int gi = uniform(s.last[which]);
+    if (gi < 0) continue;
+    const Group g = s.group[gi];
+    const int first = uniform(g.first), n = uniform(g.last) - first + 1;
+    auto slot_at = [&](int j) { return j < n ? (2 * (first + j) + (j == 0 ? 1 : 0)) * SB : kOutOfRange; };
+    const int ng = W * 64 / cols, mine = tid / cols, e4 = tid - mine * cols, h = e4 / (D / 4);
+    v4f x[8];
+    auto load8 = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(mine < ng ? j0 + i * ng + mine : n) + e4 * 16, 0, kSc1));
+    };
+    float* wt = s.part;                              // [n][G] weights
+    float* sums = wt + kKv8MaxWorkgroups * kKv8MaxG;  // [ng][G * D]
+    if (wave < G) {
+      constexpr int kRounds = kKv8MaxWorkgroups / 64;
+      float M = kLowest, L = 0.0f, low = 0.0f;
+      v2u ml[kRounds];
+#pragma unroll
+      for (int i = 0; i < kRounds; ++i)
+        if (64 * i < n) ml[i] = __builtin_amdgcn_raw_buffer_load_b64(pr, slot_at(64 * i + lane) + (G * D + 2 * wave) * 4, 0, kSc1);
+      load8(0);
+#pragma unroll
+      for (int i = 0; i < kRounds; ++i)
+        if (64 * i + lane < n) {
+          M = fmaxf(M, as_f32(ml[i].x));
+          low = fminf(low, as_f32(ml[i].y));
+        }
+      M = across_wave(M, [](float y, float z) { return fmaxf(y, z); });
+      low = across_wave(low, [](float y, float z) { return fminf(y, z); });
+#pragma unroll
+      for (int i = 0; i < kRounds; ++i)
+        if (64 * i + lane < n) {
+          const float c = ex2(as_f32(ml[i].x) - M);
+          wt[(64 * i + lane) * G + wave] = c;
+          L = __builtin_fmaf(c, as_f32(ml[i].y), L);
+        }
+      L = across_wave(L, [](float y, float z) { return y + z; });
+      if (lane == 0) s.head_l[wave] = low < 0.0f ? -1.0f : L;
+    } else {
+      load8(0);
     }
     __syncthreads();
-    float M = kLowest, L = 0.0f;
-    bool zero = false;
-    const int h = (tid % cols) / (D / 4), e4 = tid % cols, g = tid / cols, ng = W * 64 / cols;
-    for (int j = 0; j < n; ++j) {
-      M = fmaxf(M, wm[j * G + h]);
-      zero |= wl[j * G + h] < 0.0f;
-    }
-    for (int j = 0; j < n; ++j) L = __builtin_fmaf(ex2(wm[j * G + h] - M), wl[j * G + h], L);
     v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (g < ng)
-      for (int j = g; j < n; j += ng) {
-        const v4f x = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(j) + e4 * 16, 0, kSc1));
-        const float c = ex2(wm[j * G + h] - M);
+    for (int j0 = 0;;) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[e], A[e]);
+      for (int i = 0; i < 8; ++i) {
+        const int j = j0 + i * ng + mine;
+        const float c = j < n ? wt[j * G + h] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[i][e], A[e]);
       }
-    float* sums = wl + kKv8MaxWorkgroups * kKv8MaxG;  // [ng][G * D]
-    if (g < ng) *reinterpret_cast<v4f*>(sums + (g * cols + e4) * 4) = A;
+      j0 += 8 * ng;
+      if (j0 >= n) break;
+      load8(j0);
+    }
+    if (mine < ng) *reinterpret_cast<v4f*>(sums + (mine * cols + e4) * 4) = A;
     __syncthreads();
-    if (g == 0) {
+    if (mine == 0) {
       for (int j = 1; j < ng; ++j) A += *reinterpret_cast<const v4f*>(sums + (j * cols + e4) * 4);
-      const float inv = zero || L == 0.0f ? 0.0f : 1.0f / L;
-      uint16_t o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = zero ? 0 : __builtin_bit_cast(uint16_t, (_Float16)(A[e] * inv));
-      *reinterpret_cast<v2u*>(a.out + (size_t)seg * G * D + 4 * e4) = __builtin_bit_cast(v2u, o);
+      const float L = s.head_l[h];
+      store_out(a.out + (size_t)g.seg * G * D + 4 * e4, A, L, L < 0.0f);
     }
     __syncthreads();
   }
