@@ -15,6 +15,7 @@ constexpr int P = kPageSize;
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
@@ -439,22 +440,21 @@ struct Pair {
   v4f ks[2], vs[2];
 };
 
-// The partial states of a segment in a workgroup: entries at .. at + n - 1 of Lds::seg, those of
-// them that `valid` has.
+// The partial states of a segment in a workgroup: those entries of Lds::seg whose bits are set.
 struct Group {
-  int seg, at, n;
-  unsigned valid;
+  int seg;
+  unsigned states;
   int first, last;  // workgroups with states of the segment
 };
 
 struct Lds {
-  int pre[kMaxPlanBatch + 1];  // units before each row, for one KV head
+  int pre[kMaxPlanBatch + 64];  // units before each row, for one KV head
   int len[kMaxPlanBatch];
-  int wave_sum[W];
+  int wave_sum[W], wave_max[W];
   int seg[2 * W];    // segment of each wave's partial states (-1: none): one it continues, one it begins
   Group group[2 * W];
   int groups, last[2];
-  float head_l[kKv8MaxG];
+  float head_l[2][kKv8MaxG];
   __align__(16) float part[2 * W * (kKv8MaxG * D + 2 * kKv8MaxG)];
 };
 
@@ -482,32 +482,66 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   const int G = a.G;
   const int slot = G * D + ((2 * G + 3) / 4) * 4;  // floats of a state: acc [G][D], then (m, l) of each head
 
-  // Lengths -> units before each row (for one KV head). A length out of range counts as none.
-  {
+  auto fetch_ids = [&](int row, int p) {  // of page pairs p .. p + kIdPairs - 1, one id a lane
+    return 2 * p + lane < a.max_pages_per_row ? a.block_table[(size_t)row * a.max_pages_per_row + 2 * p + lane] : 0;
+  };
+  // A segment for each workgroup, if none is long: the ids are fetched while the lengths are.
+  const bool few = a.B * a.Hkv <= (int)gridDim.x;
+  const int own_row = few ? min((int)blockIdx.x / a.Hkv, a.B - 1) : -1;
+  const int own_ids = few ? fetch_ids(own_row, 0) : 0;
+
+  // Lengths -> units before each row (for one KV head), and the longest row's pairs. A length out of
+  // range counts as none.
+  auto length = [&](int i) {
+    const int n = a.seq_lens[i];
+    if (n >= 0 && n <= a.max_pages_per_row * P) return n;
+    if (blockIdx.x == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
+    return 0;
+  };
+  auto scan = [&](int x) {  // over the lanes, inclusive
+    x += dpp<0x111>(x);  // row_shr by 1, 2, 4, 8, then the rows' last lanes
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  };
+  if (lane < 2) s.seg[2 * wave + lane] = -1;
+  int longest;
+  if (a.B <= 64) {  // every wave for itself, all the same: no barrier
+    const int n = lane < a.B ? length(lane) : 0, c = lane < a.B ? pairs_of(n) + kSegment : 0;
+    const int sum = scan(c);
+    s.len[lane] = n;
+    s.pre[lane + 1] = sum;
+    if (lane == 0) s.pre[0] = 0;
+    longest = (int)across_wave((float)pairs_of(n), [](float x, float y) { return fmaxf(x, y); });
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  } else {
     const int per = (a.B + W * 64 - 1) / (W * 64);
-    int sum = 0;
+    int sum = 0, most = 0;
     for (int j = 0; j < per; ++j) {
       const int i = tid * per + j;
       if (i >= a.B) break;
-      int n = a.seq_lens[i];
-      if (n < 0 || n > a.max_pages_per_row * P) {
-        if (blockIdx.x == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
-        n = 0;
-      }
+      const int n = length(i);
       s.len[i] = n;
       sum += pairs_of(n) + kSegment;
+      most = max(most, pairs_of(n));
     }
-    int run = sum;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int y = __shfl(run, lane - x);
-      if (lane >= x) run += y;
+    const int run = scan(sum);
+    const float m = across_wave((float)most, [](float x, float y) { return fmaxf(x, y); });
+    if (lane == 63) {
+      s.wave_sum[wave] = run;
+      s.wave_max[wave] = (int)m;
     }
-    if (lane == 63) s.wave_sum[wave] = run;
-    if (lane < 2) s.seg[2 * wave + lane] = -1;
     __syncthreads();
     int at = run - sum;
-    for (int w = 0; w < wave; ++w) at += s.wave_sum[w];
+    longest = 0;
+    for (int w = 0; w < W; ++w) {
+      at += w < wave ? s.wave_sum[w] : 0;
+      longest = max(longest, s.wave_max[w]);
+    }
     for (int j = 0; j < per; ++j) {
       const int i = tid * per + j;
       if (i >= a.B) break;
@@ -515,11 +549,12 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       at += pairs_of(s.len[i]) + kSegment;
       if (i == a.B - 1) s.pre[a.B] = at;
     }
+    __syncthreads();
   }
-  __syncthreads();
 
+  const bool one = few && uniform(longest) <= kIdPairs;  // one segment per workgroup
   const int total = uniform(s.pre[a.B]) * a.Hkv;
-  const int nw = min((int)gridDim.x * W, total);  // waves with work
+  const int nw = one ? a.B * a.Hkv * W : min((int)gridDim.x * W, total);  // waves with work
   const int q_units = total / nw, r_units = total - q_units * nw;
   auto begin_of = [&](int w) { return w * q_units + min(w, r_units); };
   auto wave_of = [&](int u) {
@@ -531,15 +566,24 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   const int gw = uniform((int)blockIdx.x * W + wave);
   if (gw < nw) {
     // ---- the wave's segments, one after another
-    int u = begin_of(gw);
-    const int u_end = begin_of(gw + 1);
-    int row, head, off;
-    {
+    int u, u_end, row, head, off;  // units u .. u_end - 1, from pair `off` of (row, head) on
+    if (one) {
+      row = own_row;
+      head = (int)blockIdx.x - row * a.Hkv;
+      const int pairs = pairs_of(uniform(s.len[row]));
+      u = off = pairs * wave / W;
+      u_end = pairs > 0 ? pairs * (wave + 1) / W : (wave == 0 ? kSegment : 0);
+    } else {
+      u = begin_of(gw);
+      u_end = begin_of(gw + 1);
       const int x = u / a.Hkv;
-      int lo = 0, hi = a.B;  // pre[lo] <= x < pre[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s.pre[mid] <= x) lo = mid; else hi = mid;
+      int lo = 0, n = a.B;  // the last row with pre <= x
+      while (n > 1) {
+        const int step = (n + 63) >> 6, i = lane * step;
+        const bool below = i < n && s.pre[lo + i] <= x;
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(below)) - 1;
+        lo += c * step;
+        n = min(step, n - c * step);
       }
       row = uniform(lo);
       const int c = uniform(s.pre[row + 1] - s.pre[row]);
@@ -574,27 +618,32 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     // buffer's own loads only, not for all that may be under way.
     Segment ls, cs;
     int lp = 0;                            // next pair of ls to load
-    int ids = 0, ids_next = 0, ids_p = 0;  // ids of ls's pairs ids_p ..
-    int tag_row = -1, tag_p = 0;           // what ids_next holds
+    int ids = 0, ids_p = 0;                // ids of ls's pairs ids_p ..
+    int ids_next = own_ids, tag_row = own_row, tag_p = 0;  // fetched ahead: those of tag_row's pairs tag_p ..
     bool bad = false, bad_before = false;  // a bad page in ls; in cs when ls is ahead of it
     bool ahead = false;                    // ls is the segment after cs
     ls.p1 = 0;
     v4u qraw[4];
     const int myhead = col < 8 ? col : 15 - col;
-    auto fetch_ids = [&](int r, int p) {
-      tag_row = r;
-      tag_p = p;
-      return 2 * p + lane < a.max_pages_per_row ? a.block_table[(size_t)r * a.max_pages_per_row + 2 * p + lane] : 0;
-    };
     auto enter_ids = [&](int p) __attribute__((always_inline)) {
-      if (tag_row != ls.row || tag_p != p) ids_next = fetch_ids(ls.row, p);
+      if (tag_row != ls.row || p < tag_p || p >= tag_p + kIdPairs) {
+        tag_row = ls.row;
+        tag_p = p;
+        ids_next = fetch_ids(tag_row, tag_p);
+      }
       ids = ids_next;
       asm volatile("" : "+v"(ids));  // waited for here, not where each pair reads it
-      ids_p = p;
+      ids_p = tag_p;
       // what comes next: this segment's next pairs, or the next segment's first (of the next row, if
       // that is not an empty one)
-      if (p + kIdPairs < ls.p1) ids_next = fetch_ids(ls.row, p + kIdPairs);
-      else if (u < u_end) ids_next = fetch_ids(row, 0);
+      if (ids_p + kIdPairs < ls.p1) {
+        tag_p = ids_p + kIdPairs;
+        ids_next = fetch_ids(tag_row, tag_p);
+      } else if (u < u_end) {
+        tag_row = row;
+        tag_p = 0;
+        ids_next = fetch_ids(tag_row, tag_p);
+      }
     };
     auto enter_segment = [&]() __attribute__((always_inline)) {
       if (!next_segment(ls)) {
@@ -773,15 +822,17 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     if (starts >> lane & 1) {
       Group& g = s.group[__popcll(starts & ((1ull << lane) - 1))];
       const unsigned long long next = starts & ~((2ull << lane) - 1);
+      const unsigned below_next = next ? (1u << __builtin_ctzll(next)) - 1 : 0xFFFFFFFFu;
       g.seg = mine;
-      g.at = lane;
-      g.n = (next ? __builtin_ctzll(next) : 2 * W) - lane;
-      g.valid = (unsigned)(valid >> lane) & ((1u << g.n) - 1);
+      g.states = (unsigned)valid & below_next & ~((1u << lane) - 1);
+      g.first = g.last = (int)blockIdx.x;
       // the workgroups that hold states of the segment: those of its first to its last pair
       const int r = mine / a.Hkv, h = mine - r * a.Hkv;
       const int c = s.pre[r + 1] - s.pre[r], base = s.pre[r] * a.Hkv + h * c;
-      g.first = wave_of(base) / W;
-      g.last = wave_of(base + c - kSegment - 1) / W;
+      if (!one && (base < begin_of(blockIdx.x * W) || base + c - kSegment > begin_of(blockIdx.x * W + W))) {
+        g.first = wave_of(base) / W;
+        g.last = wave_of(base + c - kSegment - 1) / W;
+      }
     }
     if (lane == 0) {
       s.groups = __popcll(starts);
@@ -789,39 +840,51 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     }
   }
   __syncthreads();
-  const int cols = G * (D / 4);  // float4 columns of a state
+  const int cols = G * (D / 4);  // float4 columns of a state: at most half a workgroup's threads
   const __amdgpu_buffer_rsrc_t pr =
       __builtin_amdgcn_make_buffer_rsrc(a.partials, (short)0, 2 * kKv8MaxWorkgroups * SB, 0x00020000);
   const int groups = uniform(s.groups);
-  for (int it = tid; it < groups * cols; it += W * 64) {
-    const int gi = it / cols, e4 = it - gi * cols, h = e4 / (D / 4);
-    const Group g = s.group[gi];
-    const float* part = s.part + g.at * slot;
-    float M = kLowest, L = 0.0f;
-    bool zero = false;
-    for (int j = 0; j < g.n; ++j) {
-      if (!(g.valid >> j & 1)) continue;
-      M = fmaxf(M, part[j * slot + G * D + 2 * h]);
-      zero |= part[j * slot + G * D + 2 * h + 1] < 0.0f;
-    }
-    v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = 0; j < g.n; ++j) {
-      if (!(g.valid >> j & 1)) continue;
-      const float c = ex2(part[j * slot + G * D + 2 * h] - M);
-      const v4f x = *reinterpret_cast<const v4f*>(part + j * slot + 4 * e4);
-      L = __builtin_fmaf(c, part[j * slot + G * D + 2 * h + 1], L);
+  for (int gi = wave / (W / 2); gi < groups; gi += 2) {
+    const int e4 = tid & (W * 32 - 1), h = e4 / (D / 4);
+    const int seg = uniform(s.group[gi].seg), first = uniform(s.group[gi].first), last = uniform(s.group[gi].last);
+    const unsigned states = (unsigned)uniform((int)s.group[gi].states);
+    if (e4 < cols) {
+      v2f ml[2 * W];
+      v4f x[2 * W];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[e], A[e]);
-    }
-    if (g.first == g.last) {
-      store_out(a.out + (size_t)g.seg * G * D + 4 * e4, A, L, zero);
-    } else {
-      const int so = (2 * blockIdx.x + (g.first == (int)blockIdx.x ? 1 : 0)) * SB;
-      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, A), pr, so + e4 * 16, 0, kSc1);
-      if (e4 % (D / 4) == 0)
-        __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
+      for (int j = 0; j < 2 * W; ++j) {
+        if (!(states >> j & 1)) continue;
+        ml[j] = *reinterpret_cast<const v2f*>(s.part + j * slot + G * D + 2 * h);
+        x[j] = *reinterpret_cast<const v4f*>(s.part + j * slot + 4 * e4);
+      }
+      float M = kLowest, L = 0.0f;
+      bool zero = false;
+#pragma unroll
+      for (int j = 0; j < 2 * W; ++j) {
+        if (!(states >> j & 1)) continue;
+        M = fmaxf(M, ml[j].x);
+        zero |= ml[j].y < 0.0f;
+      }
+      v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < 2 * W; ++j) {
+        if (!(states >> j & 1)) continue;
+        const float c = ex2(ml[j].x - M);
+        L = __builtin_fmaf(c, ml[j].y, L);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[j][e], A[e]);
+      }
+      if (first == last) {
+        store_out(a.out + (size_t)seg * G * D + 4 * e4, A, L, zero);
+      } else {
+        const int so = (2 * blockIdx.x + (first == (int)blockIdx.x ? 1 : 0)) * SB;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, A), pr, so + e4 * 16, 0, kSc1);
+        if (e4 % (D / 4) == 0)
+          __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
+      }
     }
   }
+  if (one) return;
 
   // ---- completion count of the (at most two) segments that cross into other workgroups
   __builtin_amdgcn_s_waitcnt(0);
@@ -839,57 +902,61 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   }
   __syncthreads();
 
-  // ---- merge of a segment whose last state this workgroup brought. Threads take float4 columns,
-  // 16 / G of them a column, which share the states in turn; wave h makes the weights of head h.
-  for (int which = 0; which < 2; ++which) {
-    const int gi = uniform(s.last[which]);
-    if (gi < 0) continue;
-    const Group g = s.group[gi];
-    const int first = uniform(g.first), n = uniform(g.last) - first + 1;
-    auto slot_at = [&](int j) { return j < n ? (2 * (first + j) + (j == 0 ? 1 : 0)) * SB : kOutOfRange; };
-    const int ng = W * 64 / cols, mine = tid / cols, e4 = tid - mine * cols, h = e4 / (D / 4);
-    v4f x[8];
-    auto load8 = [&](int j0) __attribute__((always_inline)) {
+  // ---- merge of the segments whose last state this workgroup brought, by half of it each if there
+  // are two. The states of a column of four values are summed in `ng` runs (every ng-th state one
+  // run, whether a whole workgroup has the segment or half of one: the order of sums is the same),
+  // the runs then in order. The waves make the weights of a head each.
+  const int found0 = uniform(s.last[0]), found1 = uniform(s.last[1]);
+  if (found0 < 0 && found1 < 0) return;
+  const bool two = found0 >= 0 && found1 >= 0;
+  const int team = two ? wave / (W / 2) : 0, threads = two ? W * 32 : W * 64;
+  const int gi = team == 1 || found0 < 0 ? found1 : found0;
+  const int seg = uniform(s.group[gi].seg), first = uniform(s.group[gi].first), n = uniform(s.group[gi].last) - first + 1;
+  auto slot_at = [&](int j) { return j < n ? (2 * (first + j) + (j == 0 ? 1 : 0)) * SB : kOutOfRange; };
+  const int ttid = tid - team * (W * 32);
+  const int ng = W * 64 / cols, per = threads / cols, mine = ttid / cols, e4 = ttid - mine * cols, h = e4 / (D / 4);
+  v4f x[8];
+  auto load8 = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(mine < ng ? j0 + i * ng + mine : n) + e4 * 16, 0, kSc1));
-    };
-    float* wt = s.part;                              // [n][G] weights
-    float* sums = wt + kKv8MaxWorkgroups * kKv8MaxG;  // [ng][G * D]
-    if (wave < G) {
-      constexpr int kRounds = kKv8MaxWorkgroups / 64;
-      float M = kLowest, L = 0.0f, low = 0.0f;
-      v2u ml[kRounds];
+    for (int i = 0; i < 8; ++i)
+      x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(mine < per ? j0 + i * ng : n) + e4 * 16, 0, kSc1));
+  };
+  float* wt = s.part + team * (kKv8MaxWorkgroups * kKv8MaxG);                     // [n][G] weights
+  float* sums = s.part + 2 * kKv8MaxWorkgroups * kKv8MaxG + team * (W * 64 * 4);  // [ng][G * D]
+  load8(mine);
+  for (int hh = wave - team * (W / 2); hh < G; hh += threads / 64) {
+    constexpr int kRounds = kKv8MaxWorkgroups / 64;
+    v2u ml[kRounds];
+    float M = kLowest, L = 0.0f, low = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kRounds; ++i)
-        if (64 * i < n) ml[i] = __builtin_amdgcn_raw_buffer_load_b64(pr, slot_at(64 * i + lane) + (G * D + 2 * wave) * 4, 0, kSc1);
-      load8(0);
+    for (int i = 0; i < kRounds; ++i)
+      if (64 * i < n) ml[i] = __builtin_amdgcn_raw_buffer_load_b64(pr, slot_at(64 * i + lane) + (G * D + 2 * hh) * 4, 0, kSc1);
 #pragma unroll
-      for (int i = 0; i < kRounds; ++i)
-        if (64 * i + lane < n) {
-          M = fmaxf(M, as_f32(ml[i].x));
-          low = fminf(low, as_f32(ml[i].y));
-        }
-      M = across_wave(M, [](float y, float z) { return fmaxf(y, z); });
-      low = across_wave(low, [](float y, float z) { return fminf(y, z); });
+    for (int i = 0; i < kRounds; ++i)
+      if (64 * i + lane < n) {
+        M = fmaxf(M, as_f32(ml[i].x));
+        low = fminf(low, as_f32(ml[i].y));
+      }
+    M = across_wave(M, [](float y, float z) { return fmaxf(y, z); });
+    low = across_wave(low, [](float y, float z) { return fminf(y, z); });
 #pragma unroll
-      for (int i = 0; i < kRounds; ++i)
-        if (64 * i + lane < n) {
-          const float c = ex2(as_f32(ml[i].x) - M);
-          wt[(64 * i + lane) * G + wave] = c;
-          L = __builtin_fmaf(c, as_f32(ml[i].y), L);
-        }
-      L = across_wave(L, [](float y, float z) { return y + z; });
-      if (lane == 0) s.head_l[wave] = low < 0.0f ? -1.0f : L;
-    } else {
-      load8(0);
-    }
-    __syncthreads();
+    for (int i = 0; i < kRounds; ++i)
+      if (64 * i + lane < n) {
+        const float c = ex2(as_f32(ml[i].x) - M);
+        wt[(64 * i + lane) * G + hh] = c;
+        L = __builtin_fmaf(c, as_f32(ml[i].y), L);
+      }
+    L = across_wave(L, [](float y, float z) { return y + z; });
+    if (lane == 0) s.head_l[team][hh] = low < 0.0f ? -1.0f : L;
+  }
+  __syncthreads();
+  for (int run = mine; run < ng && mine < per; run += per) {
+    if (run != mine) load8(run);
     v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j0 = 0;;) {
+    for (int j0 = run;;) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int j = j0 + i * ng + mine;
+        const int j = j0 + i * ng;
         const float c = j < n ? wt[j * G + h] : 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[i][e], A[e]);
@@ -898,14 +965,14 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       if (j0 >= n) break;
       load8(j0);
     }
-    if (mine < ng) *reinterpret_cast<v4f*>(sums + (mine * cols + e4) * 4) = A;
-    __syncthreads();
-    if (mine == 0) {
-      for (int j = 1; j < ng; ++j) A += *reinterpret_cast<const v4f*>(sums + (j * cols + e4) * 4);
-      const float L = s.head_l[h];
-      store_out(a.out + (size_t)g.seg * G * D + 4 * e4, A, L, L < 0.0f);
-    }
-    __syncthreads();
+    *reinterpret_cast<v4f*>(sums + (run * cols + e4) * 4) = A;
+  }
+  __syncthreads();
+  if (mine == 0) {
+    v4f A = *reinterpret_cast<const v4f*>(sums + e4 * 4);
+    for (int j = 1; j < ng; ++j) A += *reinterpret_cast<const v4f*>(sums + (j * cols + e4) * 4);
+    const float L = s.head_l[team][h];
+    store_out(a.out + (size_t)seg * G * D + 4 * e4, A, L, L < 0.0f);
   }
 }
 
@@ -925,9 +992,11 @@ int device_units() {
 }  // namespace
 
 hipError_t launch_kv8_decode(const Kv8DecodeArgs& a, int format, hipStream_t s) {
-  // One workgroup per compute unit, fewer when the block table cannot hold as many units of work.
+  // One workgroup per compute unit, fewer where the block table cannot hold as many units of work (but
+  // one for each segment, if there are no more).
   const long long most = (long long)a.B * a.Hkv * ((a.max_pages_per_row + 1) / 2 + kSegment);
   long long grid = (most + W - 1) / W;
+  if (grid < (long long)a.B * a.Hkv) grid = (long long)a.B * a.Hkv;
   const int cap = device_units() < kKv8MaxWorkgroups ? device_units() : kKv8MaxWorkgroups;
   if (grid > cap) grid = cap;
   if (format == PKV_KV8_INT8) hipLaunchKernelGGL(kv8_decode_kernel<Int8>, dim3((unsigned)grid), dim3(W * 64), 0, s, a);
