@@ -56,14 +56,23 @@ __device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
   return __builtin_bit_cast(b8v, v4u{a.x, a.y, b.x, b.y});
 }
 
-// All 64 lanes combined, in a fixed order.
+// The 16 lanes of a row, all 64 lanes, or the 32 of each half combined, in a fixed order.
 template <typename F>
-__device__ __forceinline__ float across_wave(float x, F f) {
+__device__ __forceinline__ float across_row(float x, F f) {
   x = f(x, as_f32((unsigned)dpp<0xB1>((int)as_u32(x))));
   x = f(x, as_f32((unsigned)dpp<0x4E>((int)as_u32(x))));
   x = f(x, as_f32((unsigned)dpp<0x141>((int)as_u32(x))));
-  x = f(x, as_f32((unsigned)dpp<0x140>((int)as_u32(x))));
-  return across_rows(x, f);
+  return f(x, as_f32((unsigned)dpp<0x140>((int)as_u32(x))));
+}
+template <typename F>
+__device__ __forceinline__ float across_wave(float x, F f) { return across_rows(across_row(x, f), f); }
+template <typename F>
+__device__ __forceinline__ float half_wave(float x, F f) {
+  x = across_row(x, f);
+  unsigned a = as_u32(x), b = a;
+  asm volatile("" : "+v"(b));
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return f(as_f32((unsigned)r[0]), as_f32((unsigned)r[1]));
 }
 
 // ---------------------------------------------------------------------------------
@@ -452,6 +461,7 @@ struct Lds {
   int len[kMaxPlanBatch];
   int wave_sum[W], wave_max[W];
   int seg[2 * W];    // segment of each wave's partial states (-1: none): one it continues, one it begins
+  int base[2 * W], pairs[2 * W];  // the segment's first unit and its pairs
   Group group[2 * W];
   int groups, last[2];
   float head_l[2][kKv8MaxG];
@@ -469,9 +479,20 @@ __device__ __forceinline__ void store_out(uint16_t* out, v4f A, float L, bool ze
   *reinterpret_cast<v2u*>(out) = __builtin_bit_cast(v2u, o);
 }
 
+// A page's K as loaded (columns below 8: token col, dims of the lower half, and token 8 + col, upper
+// half; the others: the other halves of the same tokens) into token col's lower and upper half.
+__device__ __forceinline__ void sort_rows(v4u (&k)[2], int col) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned own = col < 8 ? k[0][e] : k[1][e], other = col < 8 ? k[1][e] : k[0][e];
+    k[0][e] = own;
+    k[1][e] = (unsigned)dpp<0x128>((int)other);  // row_ror by 8: the lane eight apart
+  }
+}
+
 // The part of a segment that a wave has: pairs p0 .. p1 - 1 of `pairs`.
 struct Segment {
-  int row, head, p0, p1, pairs, len;
+  int row, head, p0, p1, pairs, len, base;  // base: its first unit
 };
 
 template <typename F>
@@ -559,7 +580,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   auto begin_of = [&](int w) { return w * q_units + min(w, r_units); };
   auto wave_of = [&](int u) {
     const int big = r_units * (q_units + 1);
-    return u < big ? u / (q_units + 1) : r_units + (u - big) / q_units;
+    return (u < big ? 0 : r_units) + (u < big ? u : u - big) / (u < big ? q_units + 1 : q_units);
   };
   if ((int)blockIdx.x * W >= nw) return;
 
@@ -597,7 +618,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       while (u < u_end) {
         const int len = uniform(s.len[row]), pairs = pairs_of(len);
         const int n = min(pairs + kSegment - off, u_end - u);
-        g = Segment{row, head, off, min(off + n, pairs), pairs, len};
+        g = Segment{row, head, off, min(off + n, pairs), pairs, len, u - off};
         const bool first = off == 0;
         u += n;
         off = 0;
@@ -659,7 +680,9 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       for (int j = 0; j < 4; ++j) qraw[j] = *reinterpret_cast<const v4u*>(q + (j >> 1) * 64 + (j & 1) * 8);
       enter_ids(lp);
     };
-    const int k_at = col * D + grp * 16, v_at = kKv8CodeBytes + grp * (4 * D) + col * 16, s_at = kKv8ScaleAt + grp * 16;
+    // K: a load covers eight tokens' whole rows of 128 bytes, the two halves of a row in lanes eight
+    // apart (sort_rows puts them in order): by halves of sixteen rows, 2-4% of the time is lost.
+    const int k_at = (col & 7) * D + (col >> 3) * 64 + grp * 16, v_at = kKv8CodeBytes + grp * (4 * D) + col * 16, s_at = kKv8ScaleAt + grp * 16;
     auto load = [&](Pair& b) __attribute__((always_inline)) {
       const bool there = lp < ls.p1;
       const int left = there ? ls.len - lp * 2 * P : 0;  // tokens from the pair on
@@ -675,7 +698,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
             const_cast<uint8_t*>(a.cache + ((size_t)id * a.Hkv + (there ? ls.head : 0)) * kKv8Record), (short)0,
             page && good ? kKv8Record : 0, 0x00020000);
         b.k[pg][0] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at, 0, kNt);
-        b.k[pg][1] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at + 64, 0, kNt);
+        b.k[pg][1] = __builtin_amdgcn_raw_buffer_load_b128(r, (k_at ^ 64) + 8 * D, 0, kNt);
         b.ks[pg] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, s_at, 0, kNt));
         b.v[pg][0] = __builtin_amdgcn_raw_buffer_load_b128(r, v_at, 0, kNt);
         b.v[pg][1] = __builtin_amdgcn_raw_buffer_load_b128(r, v_at + 256, 0, kNt);
@@ -737,13 +760,20 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
             part[G * D + 2 * col + 1] = wrong ? -1.0f : sum;
           }
         }
-        if (lane == 0) s.seg[at] = cs.row * a.Hkv + cs.head;
+        if (lane == 0) {
+          s.seg[at] = cs.row * a.Hkv + cs.head;
+          s.base[at] = cs.base;
+          s.pairs[at] = cs.pairs;
+        }
       }
     };
     auto attend = [&](Pair& b, int pair) __attribute__((always_inline)) {
       v4f x[2];
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg) x[pg] = q.scores(b.k[pg], b.ks[pg]);
+      for (int pg = 0; pg < 2; ++pg) {
+        sort_rows(b.k[pg], col);
+        x[pg] = q.scores(b.k[pg], b.ks[pg]);
+      }
       const int left = cs.len - pair * 2 * P;
       if (left < 2 * P) {  // tokens past the row's end: no weight, whatever the record holds there
         asm volatile("");  // kept a branch: as selects in every pair it is a fifth of the arithmetic
@@ -815,23 +845,21 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   const int SB = slot * (int)sizeof(float);
   if (wave == 0) {
     const int mine = lane < 2 * W ? s.seg[lane] : -1;
-    const unsigned long long valid = __builtin_amdgcn_ballot_w64(mine >= 0);
-    const unsigned long long below = valid & ((1ull << lane) - 1);
-    const int prev = __shfl(mine, below ? 63 - __builtin_clzll(below) : 0);
-    const unsigned long long starts = __builtin_amdgcn_ballot_w64(mine >= 0 && (!below || prev != mine));
-    if (starts >> lane & 1) {
-      Group& g = s.group[__popcll(starts & ((1ull << lane) - 1))];
-      const unsigned long long next = starts & ~((2ull << lane) - 1);
-      const unsigned below_next = next ? (1u << __builtin_ctzll(next)) - 1 : 0xFFFFFFFFu;
+    const unsigned valid = (unsigned)__builtin_amdgcn_ballot_w64(mine >= 0);
+    const unsigned below = lane < 2 * W ? valid & ((1u << lane) - 1) : 0;
+    const int prev = __shfl(mine, below ? 31 - __builtin_clz(below) : 0);
+    const unsigned starts = (unsigned)__builtin_amdgcn_ballot_w64(mine >= 0 && (!below || prev != mine));
+    if (lane < 2 * W && (starts >> lane & 1)) {
+      Group& g = s.group[__popcll(starts & ((1u << lane) - 1))];
+      const unsigned next = starts & ~((2u << lane) - 1);
+      const int base = s.base[lane], end = base + s.pairs[lane];
       g.seg = mine;
-      g.states = (unsigned)valid & below_next & ~((1u << lane) - 1);
+      g.states = valid & (next ? (1u << __builtin_ctz(next)) - 1 : 0xFFFFFFFFu) & ~((1u << lane) - 1);
       g.first = g.last = (int)blockIdx.x;
       // the workgroups that hold states of the segment: those of its first to its last pair
-      const int r = mine / a.Hkv, h = mine - r * a.Hkv;
-      const int c = s.pre[r + 1] - s.pre[r], base = s.pre[r] * a.Hkv + h * c;
-      if (!one && (base < begin_of(blockIdx.x * W) || base + c - kSegment > begin_of(blockIdx.x * W + W))) {
+      if (!one && (base < begin_of(blockIdx.x * W) || end > begin_of(blockIdx.x * W + W))) {
         g.first = wave_of(base) / W;
-        g.last = wave_of(base + c - kSegment - 1) / W;
+        g.last = wave_of(end - 1) / W;
       }
     }
     if (lane == 0) {
@@ -840,48 +868,49 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     }
   }
   __syncthreads();
-  const int cols = G * (D / 4);  // float4 columns of a state: at most half a workgroup's threads
+  // Whole waves take a segment, 32 lanes a head, four values a lane; as many side by side as there
+  // are waves for. Lane j of a head's 32 makes the weight of state j.
+  const int cols = G * (D / 4);  // float4 columns of a state
+  const int team_waves = (cols + 63) / 64;
   const __amdgpu_buffer_rsrc_t pr =
       __builtin_amdgcn_make_buffer_rsrc(a.partials, (short)0, 2 * kKv8MaxWorkgroups * SB, 0x00020000);
-  const int groups = uniform(s.groups);
-  for (int gi = wave / (W / 2); gi < groups; gi += 2) {
-    const int e4 = tid & (W * 32 - 1), h = e4 / (D / 4);
+  const int groups = uniform(s.groups), teams = W / team_waves, my_team = wave / team_waves;
+  for (int gi = my_team; gi < groups && my_team < teams; gi += teams) {
+    const int e4 = (wave - my_team * team_waves) * 64 + lane, h = e4 / (D / 4), hl = lane & 31;
     const int seg = uniform(s.group[gi].seg), first = uniform(s.group[gi].first), last = uniform(s.group[gi].last);
     const unsigned states = (unsigned)uniform((int)s.group[gi].states);
-    if (e4 < cols) {
-      v2f ml[2 * W];
-      v4f x[2 * W];
+    const bool in = e4 < cols;
+    const bool has = in && hl < 2 * W && (states >> hl & 1);
+    const v2f ml = has ? *reinterpret_cast<const v2f*>(s.part + hl * slot + G * D + 2 * h) : v2f{kLowest, 0.0f};
+    const float M = half_wave(ml.x, [](float y, float z) { return fmaxf(y, z); });
+    const bool zero = half_wave(ml.y, [](float y, float z) { return fminf(y, z); }) < 0.0f;
+    const float c = ex2(ml.x - M);
+    const float L = half_wave(c * ml.y, [](float y, float z) { return y + z; });
+    v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (unsigned todo = states; todo != 0;) {
+      v4f x[4];
+      float w[4];
 #pragma unroll
-      for (int j = 0; j < 2 * W; ++j) {
-        if (!(states >> j & 1)) continue;
-        ml[j] = *reinterpret_cast<const v2f*>(s.part + j * slot + G * D + 2 * h);
-        x[j] = *reinterpret_cast<const v4f*>(s.part + j * slot + 4 * e4);
+      for (int i = 0; i < 4; ++i) {  // past the last one: its weight is that of a state that is not
+        const int j = todo ? __builtin_ctz(todo) : 31;
+        todo &= todo - 1;
+        x[i] = *reinterpret_cast<const v4f*>(s.part + min(j, 2 * W - 1) * slot + (in ? 4 * e4 : 0));
+        w[i] = __shfl(c, (lane & 32) + j);
+        if (j == 31) x[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
       }
-      float M = kLowest, L = 0.0f;
-      bool zero = false;
 #pragma unroll
-      for (int j = 0; j < 2 * W; ++j) {
-        if (!(states >> j & 1)) continue;
-        M = fmaxf(M, ml[j].x);
-        zero |= ml[j].y < 0.0f;
-      }
-      v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 2 * W; ++j) {
-        if (!(states >> j & 1)) continue;
-        const float c = ex2(ml[j].x - M);
-        L = __builtin_fmaf(c, ml[j].y, L);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[j][e], A[e]);
-      }
-      if (first == last) {
-        store_out(a.out + (size_t)seg * G * D + 4 * e4, A, L, zero);
-      } else {
-        const int so = (2 * blockIdx.x + (first == (int)blockIdx.x ? 1 : 0)) * SB;
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, A), pr, so + e4 * 16, 0, kSc1);
-        if (e4 % (D / 4) == 0)
-          __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
-      }
+        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(w[i], x[i][e], A[e]);
+    }
+    if (!in) continue;
+    if (first == last) {
+      store_out(a.out + (size_t)seg * G * D + 4 * e4, A, L, zero);
+    } else {
+      const int so = (2 * blockIdx.x + (first == (int)blockIdx.x ? 1 : 0)) * SB;
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, A), pr, so + e4 * 16, 0, kSc1);
+      if (hl == 0)
+        __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
     }
   }
   if (one) return;
@@ -915,22 +944,32 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   auto slot_at = [&](int j) { return j < n ? (2 * (first + j) + (j == 0 ? 1 : 0)) * SB : kOutOfRange; };
   const int ttid = tid - team * (W * 32);
   const int ng = W * 64 / cols, per = threads / cols, mine = ttid / cols, e4 = ttid - mine * cols, h = e4 / (D / 4);
-  v4f x[8];
-  auto load8 = [&](int j0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(mine < per ? j0 + i * ng : n) + e4 * 16, 0, kSc1));
+  auto load = [&](int j) __attribute__((always_inline)) {
+    return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(pr, slot_at(mine < per ? j : n) + e4 * 16, 0, kSc1));
   };
+  // The first sixteen states of the run, or the first eight of two runs, behind the loads of the first
+  // maxima and sums.
+  v4f x[16];
+  auto preload = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j0 = (two ? i & 7 : i) * ng;
+      if (j0 < n) x[i] = load(two && i >= 8 ? mine + per + j0 : mine + j0);
+      else x[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  };
+  const int head0 = wave - team * (W / 2);
+  if (head0 >= G) preload();
   float* wt = s.part + team * (kKv8MaxWorkgroups * kKv8MaxG);                     // [n][G] weights
   float* sums = s.part + 2 * kKv8MaxWorkgroups * kKv8MaxG + team * (W * 64 * 4);  // [ng][G * D]
-  load8(mine);
-  for (int hh = wave - team * (W / 2); hh < G; hh += threads / 64) {
+  for (int hh = head0; hh < G; hh += threads / 64) {
     constexpr int kRounds = kKv8MaxWorkgroups / 64;
     v2u ml[kRounds];
     float M = kLowest, L = 0.0f, low = 0.0f;
 #pragma unroll
     for (int i = 0; i < kRounds; ++i)
       if (64 * i < n) ml[i] = __builtin_amdgcn_raw_buffer_load_b64(pr, slot_at(64 * i + lane) + (G * D + 2 * hh) * 4, 0, kSc1);
+    if (hh == head0) preload();
 #pragma unroll
     for (int i = 0; i < kRounds; ++i)
       if (64 * i + lane < n) {
@@ -951,19 +990,29 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   }
   __syncthreads();
   for (int run = mine; run < ng && mine < per; run += per) {
-    if (run != mine) load8(run);
     v4f A = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j0 = run;;) {
+    auto add = [&](int j, v4f y) __attribute__((always_inline)) {
+      const float c = j < n ? wt[j * G + h] : 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int j = j0 + i * ng;
-        const float c = j < n ? wt[j * G + h] : 0.0f;
+      for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, y[e], A[e]);
+    };
+    int j = run;
+    if (run == mine || run == mine + per) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(c, x[i][e], A[e]);
+      for (int i = 0; i < 8; ++i) add(j + i * ng, run == mine ? x[i] : x[i + 8]);
+      j += 8 * ng;
+      if (!two) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add(j + i * ng, x[i + 8]);
+        j += 8 * ng;
       }
-      j0 += 8 * ng;
-      if (j0 >= n) break;
-      load8(j0);
+    }
+    for (; j < n; j += 4 * ng) {
+      v4f y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = load(j + i * ng);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add(j + i * ng, y[i]);
     }
     *reinterpret_cast<v4f*>(sums + (run * cols + e4) * 4) = A;
   }
