@@ -394,26 +394,38 @@ class DecodeBuffers:
 
 # ---- 8-bit paged KV cache (see include/pkv.h)
 
+_record_bytes = {}  # by d
+
+
 def pkv_kv8_record_bytes(d: int) -> int:
-    return int(lib().pkv_kv8_record_bytes(d))
+    n = _record_bytes.get(d)
+    if n is None:
+        n = _record_bytes[d] = int(lib().pkv_kv8_record_bytes(d))
+    return n
 
 
 def pkv_kv8_workspace_size(B: int, Hq: int, Hkv: int, d: int) -> int:
     return int(lib().pkv_kv8_workspace_size(B, Hq, Hkv, d))
 
 
-def _one_device(device: int, stream, **tensors):
+def _device_index() -> int:
+    return _current_device() if _current_device is not None else torch.cuda.current_device()
+
+
+def _one_device(stream, **tensors):
     """The tensors of a call belong on one device, the current one unless a stream is given: a
     kernel of another device's stream would read memory that is not its own."""
-    for name, t in tensors.items():
-        if t is not None and t.device.index != device:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on device {device}")
-    if stream is None and device != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
+    devices = {name: t.get_device() for name, t in tensors.items() if t is not None}
+    first = next(iter(devices.values()))
+    for name, i in devices.items():
+        if i != first:
+            raise ValueError(f"{name} is on device {i}, the other tensors on device {first}")
+    if stream is None and first != _device_index():
+        raise ValueError(f"the tensors are on device {first}, the current device is {_device_index()}")
 
 
-def _rows(t: torch.Tensor, name: str) -> tuple:
-    """(pointer, halves between tokens) of fp16 [tokens, heads, d] whose heads lie one after another."""
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Halves between tokens of fp16 [tokens, heads, d] whose heads lie one after another."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.dtype is not torch.float16:
@@ -421,32 +433,59 @@ def _rows(t: torch.Tensor, name: str) -> tuple:
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, d]")
     n, heads, d = t.shape
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (heads > 1 and s1 != d):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * d
+    return s0 if n > 1 else heads * d
 
 
-def _pool(cache: torch.Tensor, d: int) -> tuple:
-    ptr = _dev(cache, torch.uint8, "cache")
+def _explain_cache(cache, block_table, seq_lens, ws, d: int, heads=None):
+    """Raises what is wrong with a call's pool, table, lengths or workspace, if anything is."""
+    _dev(cache, torch.uint8, "cache")
     if cache.dim() != 3 or cache.shape[2] != pkv_kv8_record_bytes(d):
         raise ValueError(f"cache must be [num_pages, Hkv, {pkv_kv8_record_bytes(d)}]")
-    return ptr, cache.shape[0], cache.shape[1]
-
-
-def _table(block_table: torch.Tensor, seq_lens: torch.Tensor) -> tuple:
-    bt, lens = _dev(block_table, torch.int32, "block_table"), _dev(seq_lens, torch.int32, "seq_lens")
+    if heads is not None and cache.shape[1] != heads:
+        raise ValueError(f"cache holds {cache.shape[1]} KV heads, k has {heads}")
+    _dev(block_table, torch.int32, "block_table")
+    _dev(seq_lens, torch.int32, "seq_lens")
     if block_table.dim() != 2 or seq_lens.dim() != 1 or block_table.shape[0] != seq_lens.shape[0]:
         raise ValueError("block_table must be [B, max_pages_per_row] and seq_lens [B]")
-    return bt, block_table.shape[1], lens, seq_lens.shape[0]
+    _dev(ws, torch.uint8, "ws")
 
 
-def _offsets(offsets, B: int) -> int:
-    if offsets is None:
-        return 0
-    ptr = _dev(offsets, torch.int32, "offsets")
-    if offsets.numel() != B + 1:
-        raise ValueError("offsets must be [B + 1]")
-    return ptr
+def _explain_offsets(offsets, B: int):
+    if offsets is not None:
+        _dev(offsets, torch.int32, "offsets")
+        if offsets.numel() != B + 1:
+            raise ValueError("offsets must be [B + 1]")
+
+
+# The checks of these calls are one expression each, since a call is often shorter than a dozen
+# microseconds; where it fails, the _explain functions say what is wrong.
+
+def _move(k, v, cache, block_table, seq_lens, ws, offsets, stream):
+    """Checks of append and gather; (k, v, strides, offsets, tokens) and (num_pages, table, ...) as
+    the C calls take them."""
+    ks, vs = _rows(k, "k"), _rows(v, "v")
+    tokens, hkv, d = shape = k.shape
+    if v.shape != shape:
+        raise ValueError("k and v must have one shape")
+    dev, i32, u8 = k.get_device(), torch.int32, torch.uint8
+    pool, table = cache.shape, block_table.shape
+    B = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+    if not (len(pool) == 3 and pool[1] == hkv and pool[2] == pkv_kv8_record_bytes(d) and len(table) == 2 and table[0] == B
+            and cache.dtype is u8 and block_table.dtype is i32 and seq_lens.dtype is i32 and ws.dtype is u8
+            and cache.is_contiguous() and block_table.is_contiguous() and seq_lens.is_contiguous() and ws.is_contiguous()
+            and dev == v.get_device() == cache.get_device() == block_table.get_device() == seq_lens.get_device() == ws.get_device()
+            and (offsets is None or (offsets.dtype is i32 and offsets.numel() == B + 1 and offsets.is_contiguous()
+                                     and offsets.get_device() == dev))
+            and (stream is not None or dev == _device_index())):
+        _explain_cache(cache, block_table, seq_lens, ws, d, hkv)
+        _explain_offsets(offsets, B)
+        _one_device(stream, k=k, v=v, cache=cache, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
+    return ((k.data_ptr(), v.data_ptr(), ks, vs, 0 if offsets is None else offsets.data_ptr(), tokens),
+            (cache.data_ptr(), pool[0], block_table.data_ptr(), table[1], seq_lens.data_ptr()),
+            (B, hkv, d), (ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def pkv_kv8_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor,
@@ -454,52 +493,46 @@ def pkv_kv8_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_
     """Quantise k, v fp16 [tokens, Hkv, d] (slices of a fused projection are fine) into the pages of
     their rows, as each row's last tokens; seq_lens are the lengths after it. offsets: int32 [B + 1]
     into the tokens, or None for one token per row."""
-    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
-    if k.shape != v.shape:
-        raise ValueError("k and v must have one shape")
-    tokens, hkv, d = k.shape
-    cp, num_pages, heads = _pool(cache, d)
-    if heads != hkv:
-        raise ValueError(f"cache holds {heads} KV heads, k has {hkv}")
-    bt, maxp, lens, B = _table(block_table, seq_lens)
-    off, wp = _offsets(offsets, B), _dev(ws, torch.uint8, "ws")
-    _one_device(cache.device.index, stream, k=k, v=v, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
-    _check("pkv_kv8_append", lib().pkv_kv8_append(kp, vp, ks, vs, off, tokens, cp, num_pages, bt, maxp, lens, B, hkv, d,
-                                                  format, wp, ws.numel(), _stream(stream)))
+    moved, pool, sizes, end = _move(k, v, cache, block_table, seq_lens, ws, offsets, stream)
+    st = lib().pkv_kv8_append(*moved, *pool, *sizes, format, *end)
+    if st != PKV_OK:
+        _check("pkv_kv8_append", st)
 
 
 def pkv_kv8_gather(cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor,
                    v: torch.Tensor, ws: torch.Tensor, *, format: int, offsets=None, stream=None):
     """Read each row's last tokens back into k, v fp16 [tokens, Hkv, d]; offsets as for
     pkv_kv8_append. seq_lens[i] is where the interval ends, so any interval can be read."""
-    (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
-    if k.shape != v.shape:
-        raise ValueError("k and v must have one shape")
-    tokens, hkv, d = k.shape
-    cp, num_pages, heads = _pool(cache, d)
-    if heads != hkv:
-        raise ValueError(f"cache holds {heads} KV heads, k has {hkv}")
-    bt, maxp, lens, B = _table(block_table, seq_lens)
-    off, wp = _offsets(offsets, B), _dev(ws, torch.uint8, "ws")
-    _one_device(cache.device.index, stream, k=k, v=v, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
-    _check("pkv_kv8_gather", lib().pkv_kv8_gather(cp, num_pages, bt, maxp, lens, off, tokens, B, hkv, d, format, kp, vp,
-                                                  ks, vs, wp, ws.numel(), _stream(stream)))
+    (kp, vp, ks, vs, off, tokens), pool, sizes, end = _move(k, v, cache, block_table, seq_lens, ws, offsets, stream)
+    st = lib().pkv_kv8_gather(*pool, off, tokens, *sizes, format, kp, vp, ks, vs, *end)
+    if st != PKV_OK:
+        _check("pkv_kv8_gather", st)
 
 
 def pkv_kv8_decode(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
                    sm_scale: float, out: torch.Tensor, ws: torch.Tensor, *, format: int, stream=None):
     """Attention of one token per row over an 8-bit cache, in one launch: q, out fp16 [B, Hq, d] (q
     may be a slice of a fused projection)."""
-    qp, qs = _rows(q, "q")
-    B, hq, d = q.shape
-    cp, num_pages, hkv = _pool(cache, d)
-    bt, maxp, lens, rows = _table(block_table, seq_lens)
-    op, wp = _dev(out, torch.float16, "out"), _dev(ws, torch.uint8, "ws")
-    if rows != B or out.shape != q.shape:
-        raise ValueError("q and out must be [B, Hq, d] with the block table's B")
-    _one_device(cache.device.index, stream, q=q, block_table=block_table, seq_lens=seq_lens, out=out, ws=ws)
-    _check("pkv_kv8_decode", lib().pkv_kv8_decode(qp, qs, cp, num_pages, bt, maxp, lens, B, hq, hkv, d, format,
-                                                  float(sm_scale), op, wp, ws.numel(), _stream(stream)))
+    qs = _rows(q, "q")
+    B, hq, d = shape = q.shape
+    dev, i32, u8 = q.get_device(), torch.int32, torch.uint8
+    pool, table = cache.shape, block_table.shape
+    if not (len(pool) == 3 and pool[2] == pkv_kv8_record_bytes(d) and len(table) == 2 and table[0] == B and seq_lens.shape == (B,)
+            and out.shape == shape and out.dtype is torch.float16 and out.is_contiguous()
+            and cache.dtype is u8 and block_table.dtype is i32 and seq_lens.dtype is i32 and ws.dtype is u8
+            and cache.is_contiguous() and block_table.is_contiguous() and seq_lens.is_contiguous() and ws.is_contiguous()
+            and dev == cache.get_device() == block_table.get_device() == seq_lens.get_device() == out.get_device() == ws.get_device()
+            and (stream is not None or dev == _device_index())):
+        _explain_cache(cache, block_table, seq_lens, ws, d)
+        _dev(out, torch.float16, "out")
+        if table[0] != B or out.shape != shape:
+            raise ValueError("q and out must be [B, Hq, d] with the block table's B")
+        _one_device(stream, q=q, cache=cache, block_table=block_table, seq_lens=seq_lens, out=out, ws=ws)
+    st = lib().pkv_kv8_decode(q.data_ptr(), qs, cache.data_ptr(), pool[0], block_table.data_ptr(), table[1],
+                              seq_lens.data_ptr(), B, hq, pool[1], d, format, sm_scale, out.data_ptr(), ws.data_ptr(),
+                              ws.numel(), _stream(stream))
+    if st != PKV_OK:
+        _check("pkv_kv8_decode", st)
 
 
 def kv8_pool(num_pages: int, Hkv: int, d: int, device) -> torch.Tensor:

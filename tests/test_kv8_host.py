@@ -85,15 +85,21 @@ def test_binding_refuses_host_tensors_types_and_shapes():
         b._rows(dev((2, 8, 128), stride=(1024, 1, 8)), "k")
     with pytest.raises(ValueError, match="tokens"):
         b._rows(dev((8, 128)), "k")
-    assert b._rows(dev((2, 8, 128), stride=(6144, 128, 1)), "k")[1] == 6144
-    assert b._rows(dev((1, 8, 128), stride=(8, 128, 1)), "k")[1] == 1024   # one token: its stride says nothing
-    assert b._rows(dev((3, 1, 128), stride=(512, 5, 1)), "k")[1] == 512    # one head: likewise
-    with pytest.raises(ValueError, match="cache"):
-        b._pool(dev((4, 8, 4096), torch.uint8), 128)
-    with pytest.raises(ValueError, match="block_table"):
-        b._table(dev((3, 8), torch.int32), dev((2,), torch.int32))
+    assert b._rows(dev((2, 8, 128), stride=(6144, 128, 1)), "k") == 6144
+    assert b._rows(dev((1, 8, 128), stride=(8, 128, 1)), "k") == 1024   # one token: its stride says nothing
+    assert b._rows(dev((3, 1, 128), stride=(512, 5, 1)), "k") == 512    # one head: likewise
+    pool, ws = dev((4, 8, 4224), torch.uint8), dev((512,), torch.uint8)
+    table, lens = dev((2, 8), torch.int32), dev((2,), torch.int32)
+    b._explain_cache(pool, table, lens, ws, 128, 8)
+    for args, match in (((dev((4, 8, 4096), torch.uint8), table, lens, ws, 128), "cache"), ((pool, table, lens, ws, 64), "cache"),
+                        ((pool, table, lens, ws, 128, 4), "KV heads"), ((pool, dev((3, 8), torch.int32), lens, ws, 128), "block_table"),
+                        ((pool, table, dev((2, 1), torch.int32), ws, 128), "block_table")):
+        with pytest.raises(ValueError, match=match):
+            b._explain_cache(*args)
+    with pytest.raises(TypeError, match="seq_lens"):
+        b._explain_cache(pool, table, dev((2,), torch.int64), ws, 128)
     with pytest.raises(ValueError, match="offsets"):
-        b._offsets(dev((2,), torch.int32), 2)
+        b._explain_offsets(dev((2,), torch.int32), 2)
     with pytest.raises(ValueError, match="bad sizes"):
         pkv.Kv8Buffers(1, 72, 8, 128, "cpu")
     with pytest.raises(ValueError, match="not supported"):
@@ -102,11 +108,11 @@ def test_binding_refuses_host_tensors_types_and_shapes():
 
 def test_binding_refuses_tensors_of_several_devices(monkeypatch):
     def on(i):
-        return types.SimpleNamespace(device=types.SimpleNamespace(index=i))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    b._one_device(0, None, q=on(0), ws=on(0), offsets=None)
-    b._one_device(1, object(), q=on(1))                      # a stream is given: it says the device
+        return types.SimpleNamespace(get_device=lambda: i)
+    monkeypatch.setattr(b, "_device_index", lambda: 0)
+    b._one_device(None, q=on(0), ws=on(0), offsets=None)
+    b._one_device(object(), q=on(1))                      # a stream is given: it says the device
     with pytest.raises(ValueError, match="ws"):
-        b._one_device(0, None, q=on(0), ws=on(1))
+        b._one_device(None, q=on(0), ws=on(1))
     with pytest.raises(ValueError, match="current device"):
-        b._one_device(1, None, q=on(1))
+        b._one_device(None, q=on(1))
