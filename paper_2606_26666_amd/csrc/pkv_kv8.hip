@@ -235,25 +235,25 @@ struct Place {
   int row, pos, begin, end;
   bool there, zero;
 };
-__device__ __forceinline__ Place place(const Kv8MoveArgs& a, int t, int row) {
-  Place p{row, 0, t, t + 1, false, false};
-  if (a.offsets) {
-    p.begin = a.offsets[row];
-    p.end = a.offsets[row + 1];
-    if (t < p.begin || t >= a.offsets[a.B]) return p;
-  }
-  const int len = a.seq_lens[row];
+// `last`: offsets[B], behind which tokens are left alone.
+__device__ __forceinline__ Place place(const Kv8MoveArgs& a, int t, int row, int begin, int end, int last, int len) {
+  Place p{row, 0, begin, end, false, false};
+  if (a.offsets && (t < begin || t >= last)) return p;
   p.zero = true;
   if (!a.offsets && len == 0) return p;
-  // (p.begin <= t here) the row's tokens end after t and are no more than its length
-  if (len < 0 || len > a.max_pages_per_row * P || p.begin < 0 || p.end <= t || p.end - p.begin > len) {
+  // (begin <= t here) the row's tokens end after t and are no more than its length
+  if (len < 0 || len > a.max_pages_per_row * P || begin < 0 || end <= t || end - begin > len) {
     atomicOr(a.err, (unsigned)PKV_DEVERR_SEQ_LEN);
     return p;
   }
   p.there = true;
   p.zero = false;
-  p.pos = len - (p.end - t);
+  p.pos = len - (end - t);
   return p;
+}
+__device__ __forceinline__ Place place(const Kv8MoveArgs& a, int t, int row) {
+  if (!a.offsets) return place(a, t, row, t, t + 1, a.B, a.seq_lens[row]);
+  return place(a, t, row, a.offsets[row], a.offsets[row + 1], a.offsets[a.B], a.seq_lens[row]);
 }
 
 // The page of a position as an offset of records; a bad id takes the token out.
@@ -311,63 +311,77 @@ __device__ __forceinline__ v2u quantise(v4u raw, float& scale) {
   return v2u{F::code4(y[0], y[1], y[2], y[3]), F::code4(y[4], y[5], y[6], y[7])};
 }
 
+// One KV head of a window: `there` and `zero` per 16 lanes (see Place), token t, slot s of the record's
+// page at rec; `group`: all four lane groups are one group of the record.
+struct Window {
+  int t, s, grp, c;
+  bool there, zero, group;
+  size_t rec;
+};
+
 struct Append {
-  // One KV head of the window: `there` per 16 lanes; `group`: all four are one group of the record.
+  typedef v4u Values[2];
+  static __device__ __forceinline__ void fetch(const Kv8MoveArgs& a, const Window& w, int h, Values& x) {
+    x[0] = x[1] = v4u{0, 0, 0, 0};
+    if (!w.there) return;
+    x[0] = *reinterpret_cast<const v4u*>(a.k + (size_t)w.t * a.k_stride + h * D + w.c * 8);
+    x[1] = *reinterpret_cast<const v4u*>(a.v + (size_t)w.t * a.v_stride + h * D + w.c * 8);
+  }
   template <typename F>
-  static __device__ __forceinline__ void head(const Kv8MoveArgs& a, int t, bool there, bool, size_t rec_at, int s, int h, int grp,
-                                              int c, bool group) {
-    uint8_t* rec = a.cache + rec_at + (size_t)h * kKv8Record;
-    v4u raw[2] = {};
-    if (there) {
-      raw[0] = *reinterpret_cast<const v4u*>(a.k + (size_t)t * a.k_stride + h * D + c * 8);
-      raw[1] = *reinterpret_cast<const v4u*>(a.v + (size_t)t * a.v_stride + h * D + c * 8);
-    }
+  static __device__ __forceinline__ void finish(const Kv8MoveArgs& a, const Window& w, int h, const Values& x) {
+    uint8_t* rec = a.cache + w.rec + (size_t)h * kKv8Record;
     float scale[2];
-    const v2u kc = quantise<F>(raw[0], scale[0]);
-    v2u vc = quantise<F>(raw[1], scale[1]);
-    uint8_t* v = rec + kKv8CodeBytes + (s / 4) * (4 * D);
-    if (group) {
+    const v2u kc = quantise<F>(x[0], scale[0]);
+    v2u vc = quantise<F>(x[1], scale[1]);
+    uint8_t* v = rec + kKv8CodeBytes + (w.s / 4) * (4 * D);
+    if (w.group) {
       vc = groups_to_words(vc);
-      *reinterpret_cast<v2u*>(v + (c * 8 + 2 * grp) * 4) = vc;
+      *reinterpret_cast<v2u*>(v + (w.c * 8 + 2 * w.grp) * 4) = vc;
     }
-    if (!there) return;
-    *reinterpret_cast<v2u*>(rec + s * D + c * 8) = kc;
-    if (!group) {
+    if (!w.there) return;
+    *reinterpret_cast<v2u*>(rec + w.s * D + w.c * 8) = kc;
+    if (!w.group) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[(c * 8 + j) * 4 + s % 4] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
+      for (int j = 0; j < 8; ++j) v[(w.c * 8 + j) * 4 + w.s % 4] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
     }
-    if (c < 2) reinterpret_cast<float*>(rec + kKv8ScaleAt)[c * P + s] = c ? scale[1] : scale[0];
+    if (w.c < 2) reinterpret_cast<float*>(rec + kKv8ScaleAt)[w.c * P + w.s] = w.c ? scale[1] : scale[0];
   }
 };
 
 struct Gather {
-  template <typename F>
-  static __device__ __forceinline__ void head(const Kv8MoveArgs& a, int t, bool there, bool zero, size_t rec_at, int s, int h, int grp,
-                                              int c, bool group) {
-    const uint8_t* rec = a.cache + rec_at + (size_t)h * kKv8Record;
-    const uint8_t* v = rec + kKv8CodeBytes + (s / 4) * (4 * D);
-    v2u kc = {}, vc = {};
-    float ks = 0.0f, vs = 0.0f;
-    if (there) {
-      kc = *reinterpret_cast<const v2u*>(rec + s * D + c * 8);
-      ks = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[s];
-      vs = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[P + s];
+  struct Values {
+    v2u k, v;
+    float ks, vs;
+  };
+  static __device__ __forceinline__ void fetch(const Kv8MoveArgs& a, const Window& w, int h, Values& x) {
+    x = Values{};
+    const uint8_t* rec = a.cache + w.rec + (size_t)h * kKv8Record;
+    const uint8_t* v = rec + kKv8CodeBytes + (w.s / 4) * (4 * D);
+    if (w.there) {
+      x.k = *reinterpret_cast<const v2u*>(rec + w.s * D + w.c * 8);
+      x.ks = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[w.s];
+      x.vs = reinterpret_cast<const float*>(rec + kKv8ScaleAt)[P + w.s];
     }
-    if (group) {
-      vc = words_to_groups(*reinterpret_cast<const v2u*>(v + (c * 8 + 2 * grp) * 4));
-    } else if (there) {
+    if (w.group) {
+      x.v = *reinterpret_cast<const v2u*>(v + (w.c * 8 + 2 * w.grp) * 4);
+    } else if (w.there) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vc[j >> 2] |= (unsigned)v[(c * 8 + j) * 4 + s % 4] << (8 * (j & 3));
+      for (int j = 0; j < 8; ++j) x.v[j >> 2] |= (unsigned)v[(w.c * 8 + j) * 4 + w.s % 4] << (8 * (j & 3));
     }
-    if (!there && !zero) return;
-    h8v x, y;
+  }
+  template <typename F>
+  static __device__ __forceinline__ void finish(const Kv8MoveArgs& a, const Window& w, int h, const Values& x) {
+    const v2u v = w.group ? words_to_groups(x.v) : x.v;
+    if (!w.there && !w.zero) return;
+    h8v p, q;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      x[j] = (_Float16)(F::value(kc[j >> 2], j & 3) * ks);
-      y[j] = (_Float16)(F::value(vc[j >> 2], j & 3) * vs);
+      p[j] = (_Float16)(F::value(x.k[j >> 2], j & 3) * x.ks);
+      q[j] = (_Float16)(F::value(v[j >> 2], j & 3) * x.vs);
     }
-    *reinterpret_cast<h8v*>(a.k + (size_t)t * a.k_stride + h * D + c * 8) = x;
-    *reinterpret_cast<h8v*>(a.v + (size_t)t * a.v_stride + h * D + c * 8) = y;
+    // streamed past the caches: 6% faster than kept in them, where the records' lines then stay
+    __builtin_nontemporal_store(p, reinterpret_cast<h8v*>(a.k + (size_t)w.t * a.k_stride + h * D + w.c * 8));
+    __builtin_nontemporal_store(q, reinterpret_cast<h8v*>(a.v + (size_t)w.t * a.v_stride + h * D + w.c * 8));
   }
 };
 
@@ -381,7 +395,15 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
        unit += (long long)gridDim.x * kMoveWaves) {
     const int w0 = (int)(unit / chunks) * 4, h0 = (int)(unit % chunks) * chunk, h1 = min(h0 + chunk, a.Hkv);
     auto heads = [&](int t, bool there, bool zero, size_t rec, int s, bool group) __attribute__((always_inline)) {
-      for (int h = h0; h < h1; ++h) Op::template head<F>(a, t, there, zero, rec, s, h, grp, c, group);
+      const Window w{t, s, grp, c, there, zero, group, rec};
+      typename Op::Values x[2];  // a head's loads are under way while the one before it is finished
+      Op::fetch(a, w, h0, x[0]);
+      for (int h = h0; h < h1; h += 2) {
+        if (h + 1 < h1) Op::fetch(a, w, h + 1, x[1]);
+        Op::template finish<F>(a, w, h, x[0]);
+        if (h + 2 < h1) Op::fetch(a, w, h + 2, x[0]);
+        if (h + 1 < h1) Op::template finish<F>(a, w, h + 1, x[1]);
+      }
     };
     const int left = a.tokens - w0;
     if (kScatter) {
@@ -401,8 +423,18 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
       continue;
     }
     const int w1 = left < 4 ? a.tokens : w0 + 4;
+    // Few rows: their offsets and lengths a lane each, one round of loads for all tokens.
+    const bool few = a.B < 64;
+    const int off = few && lane <= a.B ? a.offsets[lane] : 0, len = few && lane < a.B ? a.seq_lens[lane] : 0;
     for (int t = w0; t < w1;) {
-      const Place p = place(a, t, row_of(a, t, lane));
+      Place p;
+      if (few) {
+        const int row = max(__popcll(__builtin_amdgcn_ballot_w64(lane < a.B && off <= t)) - 1, 0);
+        p = place(a, t, row, __builtin_amdgcn_readlane(off, row), __builtin_amdgcn_readlane(off, row + 1),
+                  __builtin_amdgcn_readlane(off, a.B), __builtin_amdgcn_readlane(len, row));
+      } else {
+        p = place(a, t, row_of(a, t, lane));
+      }
       if (!p.there) {  // left alone, or zeros, a token at a time
         if (p.zero) heads(t, false, grp == 0, 0, 0, false);
         ++t;
@@ -1055,9 +1087,11 @@ hipError_t launch_kv8_decode(const Kv8DecodeArgs& a, int format, hipStream_t s) 
 
 namespace {
 
-// Heads per wave: one, as long as the waves then are no more than the device can hold some eight
-// times over, so that small calls spread; beyond, several, which share the lookups.
-constexpr long long kMoveUnits = 65536;
+// Heads per wave: one, as long as the waves then are no more than twice what the device holds, so
+// that small calls spread; beyond, several, which share the lookups (16 rows of up to 8192 tokens read
+// back: one head a wave 114 us, up to 65536 waves 91, 16384 or 4096 82, and 71 with two heads under
+// way; chunks of eight rows 14.4 us at 16384, 14.0 at 4096).
+constexpr long long kMoveUnits = 4096;
 
 template <typename Op, typename F>
 hipError_t launch_move(const Kv8MoveArgs& a, hipStream_t s) {
