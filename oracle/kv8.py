@@ -59,27 +59,24 @@ def views(pool: np.ndarray):
     n, h, _ = pool.shape
     k = pool[:, :, :PAGE * D].reshape(n, h, PAGE, D)
     v = pool[:, :, PAGE * D:2 * PAGE * D].reshape(n, h, 4, D, 4)
-    s = np.ascontiguousarray(pool[:, :, 2 * PAGE * D:]).view(np.float32)
+    s = pool[:, :, 2 * PAGE * D:].view(np.float32)
     return k, v, s[:, :, :PAGE], s[:, :, PAGE:]
 
 
 def ref_append(pool, k, v, block_table, seq_lens, fmt, offsets=None) -> np.ndarray:
     """The pool after the write."""
     pool = pool.copy()
-    for x, base, sbase in ((k, 0, 2 * PAGE * D), (v, PAGE * D, 2 * PAGE * D + PAGE * 4)):
-        codes, scales = quantise(x, fmt)
-        for i, n in enumerate(np.asarray(seq_lens).tolist()):
-            b, e = (i, i + (n > 0)) if offsets is None else (int(offsets[i]), int(offsets[i + 1]))
-            for t in range(b, e):
-                pos = n - (e - t)
-                page, s = int(block_table[i, pos // PAGE]), pos % PAGE
-                for h in range(pool.shape[1]):
-                    rec = pool[page, h]
-                    if base == 0:
-                        rec[s * D:(s + 1) * D] = codes[t, h]
-                    else:
-                        rec[base + (s // 4) * 4 * D + s % 4:base + (s // 4 + 1) * 4 * D:4] = codes[t, h]
-                    rec[sbase + 4 * s:sbase + 4 * s + 4] = np.frombuffer(scales[t, h].tobytes(), dtype=np.uint8)
+    kc, vc, ks, vs = views(pool)
+    assert all(np.shares_memory(x, pool) for x in (kc, vc, ks, vs))
+    (kq, ksc), (vq, vsc) = quantise(k, fmt), quantise(v, fmt)
+    for i, n in enumerate(np.asarray(seq_lens).tolist()):
+        b, e = (i, i + (n > 0)) if offsets is None else (int(offsets[i]), int(offsets[i + 1]))
+        pos = np.arange(n - (e - b), n)
+        page, s = np.asarray(block_table[i])[pos // PAGE], pos % PAGE
+        kc[page, :, s] = kq[b:e]
+        vc[page, :, s // 4, :, s % 4] = vq[b:e]
+        ks[page, :, s] = ksc[b:e]
+        vs[page, :, s] = vsc[b:e]
     return pool
 
 

@@ -102,7 +102,7 @@ struct Int8 {
   }
   // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as three
   // balanced base-256 digits of x = round(q * 2^22 / max|q|), x = 65536 d2 + 256 d1 + d0 with d2 in
-  // [-64, 64], d1 and d0 in [-128, 127]. The sums of digits times codes are exact, and the rounding of
+  // [-64, 64], d1 and d0 in [-128, 127] (d2's and d1's borders moved up by the digits below them). The sums of digits times codes are exact, and the rounding of
   // q is 2^-23 of its largest value. First operand: d2 in column h, d1 in column 15 - h; second: d0
   // in both.
   struct Query {
@@ -120,23 +120,22 @@ struct Int8 {
       unit = top < 0x7C00u ? most * 0x1p-22f * scale : __builtin_nanf("");
       const float inv = most > 0.0f && top < 0x7C00u ? 0x1p22f / most : 0.0f;
       shift = col < 8 ? 8 : 0;
+      // 1.5 * 2^23 + q * inv, rounded once, has x in its low bits, 0x4B400000 above. A byte of x + bias
+      // is a digit: d2 = (x + 2^15 + 2^7) >> 16, d1 the low byte of (x + 2^7) >> 8, d0 that of x.
+      const unsigned bias = (col < 8 ? 0x8080u : 0x80u) - 0x400000u;
+      const unsigned low = col < 8 ? 0x0C0C0602u : 0x0C0C0501u;  // bytes 2 or 1 of a pair
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const h8v y = __builtin_bit_cast(h8v, raw[j]);
-        unsigned first[2] = {0, 0}, second[2] = {0, 0};
+        unsigned x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int x = inv > 0.0f ? (int)__builtin_rintf((float)y[e] * inv) : 0;
-          const int x1 = (x + 128) >> 8;  // x = 256 x1 + d0
-          const int x2 = (x1 + 128) >> 8;
-          const int d = col < 8 ? x2 : x1;  // d1 and d0: the low bytes of x1 and x
-          first[e >> 2] |= ((unsigned)d & 255u) << (8 * (e & 3));
-          second[e >> 2] |= ((unsigned)x & 255u) << (8 * (e & 3));
-        }
+        for (int e = 0; e < 8; ++e) x[e] = inv > 0.0f ? as_u32(__builtin_fmaf((float)y[e], inv, 12582912.0f)) : 0x4B400000u;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          b[0][j >> 1][2 * (j & 1) + i] = first[i];
-          b[1][j >> 1][2 * (j & 1) + i] = second[i];
+          const unsigned* z = x + 4 * i;
+          b[0][j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias, z[0] + bias, low) |
+                                          __builtin_amdgcn_perm(z[3] + bias, z[2] + bias, low) << 16;
+          b[1][j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1], z[0], 0x0C0C0400u) | __builtin_amdgcn_perm(z[3], z[2], 0x04000C0Cu);
         }
       }
     }
@@ -474,6 +473,12 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
 // registers and from there into the matrix cores, without LDS.
 constexpr int W = 8;        // waves of a workgroup
 constexpr int kSegment = 1;  // units of a segment beyond its pairs
+// Up to so many pairs of the longest row (half of them unless the waves have several segments each)
+// a wave takes whole segments: what it has more or less than others costs less than states that
+// meet (Hkv = 8, 256 rows of 10-60 tokens 22.5 -> 13.9 us, of 60-130 26.9 -> 22.7, of 100-250 31.6 ->
+// 28.3, of 100-400 36.8 -> 35.4; Hkv = 32, 64 rows of 100-300 30.3 -> 26.7). Beyond it does not (512 rows
+// of 100-600 tokens 78 -> 87).
+constexpr int kWhole = 16;
 constexpr int kIdPairs = 32;  // page pairs whose ids a wave holds (one id a lane)
 
 struct Pair {
@@ -614,6 +619,8 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     const int big = r_units * (q_units + 1);
     return (u < big ? 0 : r_units) + (u < big ? u : u - big) / (u < big ? q_units + 1 : q_units);
   };
+  // A wave has whole segments, those that begin in its units.
+  const bool whole = !one && uniform(longest) <= kWhole && uniform(longest) <= max(kWhole / 2, 2 * q_units);
   if ((int)blockIdx.x * W >= nw) return;
 
   const int gw = uniform((int)blockIdx.x * W + wave);
@@ -643,13 +650,21 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       const int rel = u - uniform(s.pre[row]) * a.Hkv;
       head = rel / c;
       off = rel - head * c;
+      if (whole && off > 0) {
+        u += c - off;
+        off = 0;
+        if (++head == a.Hkv) {
+          head = 0;
+          ++row;
+        }
+      }
     }
     auto out_of = [&](const Segment& g) { return a.out + ((size_t)g.row * a.Hq + (size_t)g.head * G) * D; };
     // The next segment with pairs in the wave's range; empty rows on the way are written as zeros.
     auto next_segment = [&](Segment& g) __attribute__((always_inline)) {
       while (u < u_end) {
         const int len = uniform(s.len[row]), pairs = pairs_of(len);
-        const int n = min(pairs + kSegment - off, u_end - u);
+        const int n = whole ? pairs + kSegment : min(pairs + kSegment - off, u_end - u);
         g = Segment{row, head, off, min(off + n, pairs), pairs, len, u - off};
         const bool first = off == 0;
         u += n;
@@ -871,6 +886,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       live = true;
     }
   }
+  if (whole) return;
   __syncthreads();
 
   // ---- states of segments that several waves share: runs of equal entries of s.seg

@@ -46,11 +46,23 @@ class Cache:
         bt, n = page_table(np.maximum(self.lens, 1) + 16 * (spare - 1), 16, 0.3, r)
         self.bt, self.num_pages = np.ascontiguousarray(bt, dtype=np.int32), int(n)
         self.pool = np.full((self.num_pages, hkv, kv8.RECORD), 0xFF, dtype=np.uint8)
-        if filled:
-            n = int(self.lens.sum())
-            offs = np.concatenate([[0], np.cumsum(self.lens)]).astype(np.int32)
-            k, v = (r.standard_normal((n, hkv, kv8.D)).astype(np.float16) for _ in "kv")
-            self.pool = kv8.ref_append(self.pool, k, v, self.bt, self.lens, fmt, offs)
+        if filled:  # codes and scales as values near N(0, 1) leave them
+            row = np.repeat(np.arange(self.B), self.lens)
+            pos = np.concatenate([np.arange(n) for n in self.lens] + [np.zeros(0, dtype=np.int64)]).astype(np.int64)
+            page, slot = self.bt[row, pos // 16], pos % 16
+            k, v, ks, vs = kv8.views(self.pool)
+            for codes, scales in ((k, ks), (v, vs)):
+                x = r.standard_normal((len(pos), hkv, kv8.D), dtype=np.float32)
+                if fmt == kv8.INT8:
+                    c = np.clip(np.rint(x * 40), -127, 127).astype(np.int8).view(np.uint8)
+                else:
+                    c = (np.searchsorted(kv8.VALUES[fmt][:127], np.abs(x) * 100) + 128 * (x < 0)).clip(0, 254).astype(np.uint8)
+                    c[c == 127] = 126
+                if codes.ndim == 4:
+                    codes[page, :, slot] = c
+                else:
+                    codes[page, :, slot // 4, :, slot % 4] = c
+                scales[page, :, slot] = (r.random((len(pos), hkv)) * 0.4 + 0.8) / (40 if fmt == kv8.INT8 else 100)
 
 
 def call(exe, what, cache, *, lens=None, bt=None, q=None, k=None, v=None, offsets=None, tokens=0, strides=None, hq=None,
