@@ -5,7 +5,10 @@ pages last, decode one token per step and leave when their decode length is reac
 Each step runs the attention path of this library over the whole slot batch in one
 launch (`pkv_plan_decode`: free slots have length 0 and get no tasks), optionally
 followed by a gated-MLP tail of intermediate width 11008 on the active rows (the
-model-level proxy of Sec. 4.6, dense fp16 GEMMs through torch).
+model-level proxy of Sec. 4.6, dense fp16 GEMMs through torch). With kv="int8" or "e4m3"
+the cache is held in 8 bits: a step quantises its new tokens into their pages
+(`pkv_kv8_append`) and attends over them (`pkv_kv8_decode`), and what a row holds is read
+back in fp16 (`pkv_kv8_gather`).
 
   PagePool    host free list of physical page ids, handed out in a seeded permuted
               order so that a request's pages are scattered in memory (Sec. 3.7)
@@ -30,6 +33,8 @@ from . import _binding as _b
 from . import costmodel
 
 PAGE = 16
+KV_FORMATS = {"fp16": None, "int8": _b.PKV_KV8_INT8, "e4m3": _b.PKV_KV8_E4M3}
+FILL_TOKENS = 1 << 16  # tokens quantised at a time where a pool is filled
 
 
 class PagePool:
@@ -78,7 +83,9 @@ class Engine:
 
     def __init__(self, max_batch: int, max_pages_per_row: int, num_pages: int, hq: int = 32, hkv: int = 8,
                  d: int = 128, split=(16, 64), target_tasks: int = 0, policy: int = 1, mlp: bool = False,
-                 mlp_width: int = 11008, seed: int = 0, device="cuda"):
+                 mlp_width: int = 11008, seed: int = 0, device="cuda", kv: str = "fp16"):
+        if kv not in KV_FORMATS:
+            raise ValueError(f"kv must be one of {sorted(KV_FORMATS)}, got {kv!r}")
         import torch
         self.torch = torch
         self.dev = torch.device(device)
@@ -87,16 +94,23 @@ class Engine:
         g = torch.Generator(device=self.dev)
         g.manual_seed(seed)
         self.gen = g
-        shape = (num_pages, PAGE, hkv, d)
-        self.k = torch.randn(shape, generator=g, device=self.dev, dtype=torch.float32).half()
-        self.v = torch.randn(shape, generator=g, device=self.dev, dtype=torch.float32).half()
+        self.kv, self.format = kv, KV_FORMATS[kv]
+        if self.format is None:
+            shape = (num_pages, PAGE, hkv, d)
+            self.k = torch.randn(shape, generator=g, device=self.dev, dtype=torch.float32).half()
+            self.v = torch.randn(shape, generator=g, device=self.dev, dtype=torch.float32).half()
         self.bt_host = np.zeros((max_batch, max_pages_per_row), dtype=np.int32)
         self.bt = torch.zeros((max_batch, max_pages_per_row), dtype=torch.int32, device=self.dev)
         self.lens_host = np.zeros(max_batch, dtype=np.int32)
         self.lens = torch.zeros(max_batch, dtype=torch.int32, device=self.dev)
         self.q = torch.zeros((max_batch, hq, d), dtype=torch.float16, device=self.dev)
         self.out = torch.zeros((max_batch, hq, d), dtype=torch.float16, device=self.dev)
-        self.bufs = _b.DecodeBuffers(max_batch, hq, hkv, d, split[1], self.dev)
+        if self.format is None:
+            self.bufs = _b.DecodeBuffers(max_batch, hq, hkv, d, split[1], self.dev)
+        else:
+            self.bufs = _b.Kv8Buffers(max_batch, hq, hkv, d, self.dev)
+            self.cache = _b.kv8_pool(num_pages, hkv, d, self.dev)
+            self._fill(num_pages)
         # target 0: the cost model's rule, per step, from the active rows
         self.split, self.policy, self.fixed_target = split, policy, target_tasks
         self.params = _b.make_params(hkv, split[0], split[1], target_tasks or costmodel.CUS, policy=policy)
@@ -106,6 +120,19 @@ class Engine:
             self.mlp = tuple((torch.randn(shape2, generator=g, device=self.dev, dtype=torch.float32)
                               / np.sqrt(shape2[0])).half()
                              for shape2 in ((h, mlp_width), (h, mlp_width), (mlp_width, h)))
+
+    def _new_tokens(self, n: int) -> tuple:
+        return tuple(self.torch.randn((n, self.hkv, self.d), generator=self.gen, device=self.dev).half() for _ in "kv")
+
+    def _fill(self, num_pages: int) -> None:
+        """Every page of the 8-bit pool with seeded values: a page is a row of 16 tokens."""
+        torch, at_once = self.torch, FILL_TOKENS // PAGE
+        ws = _b.Kv8Buffers(min(num_pages, at_once), self.hq, self.hkv, self.d, self.dev).ws
+        for first in range(0, num_pages, at_once):
+            ids = torch.arange(first, min(num_pages, first + at_once), dtype=torch.int32, device=self.dev)
+            k, v = self._new_tokens(ids.numel() * PAGE)
+            _b.pkv_kv8_append(k, v, self.cache, ids[:, None].contiguous(), torch.full_like(ids, PAGE), ws, format=self.format,
+                              offsets=torch.arange(0, ids.numel() + 1, dtype=torch.int32, device=self.dev) * PAGE)
 
     def admit(self, slot: int, pages, prompt_len: int) -> None:
         row = np.full(self.maxp, 0, dtype=np.int32)
@@ -128,7 +155,11 @@ class Engine:
         pages = self.bt_host[idx, pos // PAGE].astype(np.int64)
         self.lens_host[idx] += 1
         ev[0].record()
-        if idx.size:
+        if idx.size and self.format is not None:
+            k, v = self._new_tokens(self.B)      # a token for every slot; free ones are skipped
+            self.q.normal_(generator=self.gen)
+            self.q.mul_(1.0 / np.sqrt(self.d))
+        elif idx.size:
             n = idx.size
             pg = torch.from_numpy(pages).to(self.dev, non_blocking=True)
             sl = torch.from_numpy(pos % PAGE).to(self.dev, non_blocking=True)
@@ -137,11 +168,16 @@ class Engine:
             self.q.normal_(generator=self.gen)
             self.q.mul_(1.0 / np.sqrt(self.d))
         self.lens.copy_(torch.from_numpy(self.lens_host))
-        if not self.fixed_target:
-            self.params.target_tasks = costmodel.default_target(self.lens_host[idx], self.hkv, hq=self.hq)
         b = self.bufs
-        _b.pkv_plan_decode(self.q, self.k, self.v, self.bt, self.lens, self.params, b.tasks, b.split_offsets,
-                           b.num_tasks, 1.0, self.out, b.ws)
+        if self.format is None:
+            if not self.fixed_target:
+                self.params.target_tasks = costmodel.default_target(self.lens_host[idx], self.hkv, hq=self.hq)
+            _b.pkv_plan_decode(self.q, self.k, self.v, self.bt, self.lens, self.params, b.tasks, b.split_offsets,
+                               b.num_tasks, 1.0, self.out, b.ws)
+        else:
+            if idx.size:
+                _b.pkv_kv8_append(k, v, self.cache, self.bt, self.lens, b.ws, format=self.format)
+            _b.pkv_kv8_decode(self.q, self.cache, self.bt, self.lens, 1.0, self.out, b.ws, format=self.format)
         ev[1].record()
         if self.mlp is not None and idx.size:
             x = self.out[torch.from_numpy(idx).to(self.dev)].reshape(idx.size, self.hq * self.d)
@@ -157,8 +193,33 @@ class Engine:
         block_table, lens), for checking."""
         self.torch.cuda.synchronize()
         idx = np.asarray(slots, dtype=np.int64)
-        return (self.q.cpu().numpy()[idx], self.k.cpu().numpy(), self.v.cpu().numpy(),
-                self.bt_host[idx].copy(), self.lens_host[idx].copy())
+        bt, lens = self.bt_host[idx].copy(), self.lens_host[idx].copy()
+        if self.format is None:
+            k, v = self.k.cpu().numpy(), self.v.cpu().numpy()
+        else:  # the slots' tokens at their places in pools of fp16
+            k, v = (np.zeros((self.cache.shape[0], PAGE, self.hkv, self.d), dtype=np.float16) for _ in "kv")
+            row = np.repeat(np.arange(idx.size), lens)
+            pos = np.arange(row.size) - np.repeat(np.cumsum(lens) - lens, lens)
+            for pool, x in zip((k, v), self.cached(slots)):
+                pool[bt[row, pos // PAGE], pos % PAGE] = x.cpu().numpy()
+        return self.q.cpu().numpy()[idx], k, v, bt, lens
+
+    def cached(self, slots):
+        """(K, V) fp16 [tokens, hkv, d] that the 8-bit cache holds for `slots`, row after row."""
+        if self.format is None:
+            raise ValueError("the cache is not in 8 bits")
+        torch = self.torch
+        lens = np.zeros(self.B, dtype=np.int32)  # the calls' rows are the slots: others have no tokens
+        lens[np.asarray(slots, dtype=np.int64)] = self.lens_host[np.asarray(slots, dtype=np.int64)]
+        offsets = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        k, v = (torch.empty((int(offsets[-1]), self.hkv, self.d), dtype=torch.float16, device=self.dev) for _ in "kv")
+        _b.pkv_kv8_gather(self.cache, self.bt, torch.from_numpy(lens).to(self.dev), k, v, self.bufs.ws, format=self.format,
+                          offsets=torch.from_numpy(offsets).to(self.dev))
+        order = np.argsort(np.asarray(slots, dtype=np.int64), kind="stable")
+        if np.array_equal(order, np.arange(len(order))):
+            return k, v
+        parts = [slice(offsets[s], offsets[s + 1]) for s in slots]  # in the order asked for
+        return tuple(torch.cat([x[p] for p in parts]) for x in (k, v))
 
 
 class Scheduler:
@@ -250,6 +311,7 @@ def main(argv=None) -> int:
     ap.add_argument("--arrival-gap", type=int, default=0)
     ap.add_argument("--mlp", action="store_true", help="gated-MLP tail (width 11008) after attention")
     ap.add_argument("--target-tasks", type=int, default=0, help="0: the cost model's rule per step")
+    ap.add_argument("--kv", choices=sorted(KV_FORMATS), default="fp16", help="how the cache is held")
     ap.add_argument("--seed", type=int, default=20260623)
     args = ap.parse_args(argv)
     import torch
@@ -264,10 +326,11 @@ def main(argv=None) -> int:
     maxp = max(-(-(q.prompt_len + q.decode_len) // PAGE) for q in trace)
     num_pages = maxp * args.max_batch + maxp        # the batch's worst case plus one spare row
     engine = Engine(args.max_batch, maxp, num_pages, target_tasks=args.target_tasks, mlp=args.mlp,
-                    seed=args.seed)
+                    seed=args.seed, kv=args.kv)
     sched = Scheduler(trace, engine, PagePool(num_pages, args.seed), args.max_batch)
     stats = sched.run(args.steps, warmup=args.warmup)
     stats.update({"trace": args.trace, "requests": len(trace), "max_batch": args.max_batch, "mlp": args.mlp,
+                  "kv": args.kv,
                   "seed": args.seed})
     print(json.dumps(stats))
     return 0

@@ -291,3 +291,44 @@ def test_refusals():
                     (dict(offsets=torch.zeros(3, dtype=torch.int32, device=DEV)), ValueError)):
         with pytest.raises(err):
             pkv.pkv_kv8_append(**{**dict(k=k, v=k, cache=d.pool, block_table=d.bt, seq_lens=d.lens, ws=d.bufs.ws, format=0), **kw})
+
+
+@pytest.mark.parametrize("kv", ["int8", "e4m3"])
+def test_serving_over_an_8_bit_cache(kv):
+    """Requests come and go; each step appends, attends and (here) reads back, checked against the oracle
+    over what is read back: off by its fp16 rounding, half a step of K and V."""
+    from oracle import ref_decode
+    from paper_2606_26666_amd.serving import PAGE, Engine, PagePool, Scheduler
+    from tests.gpu_cases import assert_close
+    from workloads.requests import Request
+    trace = [Request(0, 0, 300, 3), Request(1, 0, 5000, 6), Request(2, 1, 1200, 2), Request(3, 2, 64, 4), Request(4, 4, 900, 2)]
+    maxp = max(-(-(q.prompt_len + q.decode_len) // PAGE) for q in trace)
+    engine = Engine(4, maxp, 4 * maxp, mlp=True, seed=7, kv=kv)
+    checked = []
+
+    def check(rec):
+        slots = rec["slots"]
+        out = engine.out.cpu()
+        if slots:
+            q, k, v, bt, lens = engine.snapshot(slots)
+            assert_close(out[slots], ref_decode(q, k, v, bt, lens), f"step {rec['step']}")
+            back = engine.cached(slots[::-1])[0]
+            n = int(lens[-1])
+            last = torch.from_numpy(k[bt[-1, (n - 1) // PAGE], (n - 1) % PAGE])
+            assert torch.equal(back[n - 1].cpu(), last)
+            checked.append(rec["step"])
+        assert torch.all(out[[s for s in range(4) if s not in slots]] == 0)
+        assert pkv.pkv_check_device_status(engine.bufs.ws) == 0
+
+    sched = Scheduler(trace, engine, PagePool(4 * maxp, seed=7), max_batch=4, observer=check)
+    while not sched.finished and sched.step_idx < 30:
+        sched.step()
+    assert sched.finished and sorted(sched.done) == list(range(5)) and len(checked) >= 6
+
+
+def test_serving_refuses_an_unknown_format():
+    from paper_2606_26666_amd.serving import Engine
+    with pytest.raises(ValueError, match="kv must be"):
+        Engine(4, 4, 16, kv="int4")
+    with pytest.raises(ValueError, match="8 bits"):
+        Engine(1, 1, 1, hq=1, hkv=1).cached([0])

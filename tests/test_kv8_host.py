@@ -116,3 +116,10 @@ def test_binding_refuses_tensors_of_several_devices(monkeypatch):
         b._one_device(None, q=on(0), ws=on(1))
     with pytest.raises(ValueError, match="current device"):
         b._one_device(None, q=on(1))
+
+
+def test_serving_names_its_formats():
+    from paper_2606_26666_amd.serving import KV_FORMATS, Engine
+    assert KV_FORMATS == {"fp16": None, "int8": pkv.PKV_KV8_INT8, "e4m3": pkv.PKV_KV8_E4M3}
+    with pytest.raises(ValueError, match="kv must be"):
+        Engine(4, 4, 16, kv="int4")
