@@ -413,15 +413,18 @@ def _device_index() -> int:
 
 
 def _one_device(stream, **tensors):
-    """The tensors of a call belong on one device, the current one unless a stream is given: a
-    kernel of another device's stream would read memory that is not its own."""
+    """The tensors of a call, and the stream if one is given, belong on the current device: a launch
+    goes there, and a kernel would read memory that is not its own."""
     devices = {name: t.get_device() for name, t in tensors.items() if t is not None}
     first = next(iter(devices.values()))
     for name, i in devices.items():
         if i != first:
             raise ValueError(f"{name} is on device {i}, the other tensors on device {first}")
-    if stream is None and first != _device_index():
+    if first != _device_index():
         raise ValueError(f"the tensors are on device {first}, the current device is {_device_index()}")
+    on = getattr(stream, "device_index", first)
+    if on != first:
+        raise ValueError(f"the stream is on device {on}, the tensors on device {first}")
 
 
 def _rows(t: torch.Tensor, name: str) -> int:
@@ -479,7 +482,7 @@ def _move(k, v, cache, block_table, seq_lens, ws, offsets, stream):
             and dev == v.get_device() == cache.get_device() == block_table.get_device() == seq_lens.get_device() == ws.get_device()
             and (offsets is None or (offsets.dtype is i32 and offsets.numel() == B + 1 and offsets.is_contiguous()
                                      and offsets.get_device() == dev))
-            and (stream is not None or dev == _device_index())):
+            and dev == _device_index() and (stream is None or getattr(stream, "device_index", dev) == dev)):
         _explain_cache(cache, block_table, seq_lens, ws, d, hkv)
         _explain_offsets(offsets, B)
         _one_device(stream, k=k, v=v, cache=cache, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
@@ -522,7 +525,7 @@ def pkv_kv8_decode(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tens
             and cache.dtype is u8 and block_table.dtype is i32 and seq_lens.dtype is i32 and ws.dtype is u8
             and cache.is_contiguous() and block_table.is_contiguous() and seq_lens.is_contiguous() and ws.is_contiguous()
             and dev == cache.get_device() == block_table.get_device() == seq_lens.get_device() == out.get_device() == ws.get_device()
-            and (stream is not None or dev == _device_index())):
+            and dev == _device_index() and (stream is None or getattr(stream, "device_index", dev) == dev)):
         _explain_cache(cache, block_table, seq_lens, ws, d)
         _dev(out, torch.float16, "out")
         if table[0] != B or out.shape != shape:

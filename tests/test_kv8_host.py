@@ -111,7 +111,12 @@ def test_binding_refuses_tensors_of_several_devices(monkeypatch):
         return types.SimpleNamespace(get_device=lambda: i)
     monkeypatch.setattr(b, "_device_index", lambda: 0)
     b._one_device(None, q=on(0), ws=on(0), offsets=None)
-    b._one_device(object(), q=on(1))                      # a stream is given: it says the device
+    b._one_device(types.SimpleNamespace(device_index=0), q=on(0))
+    b._one_device(12345, q=on(0))                         # a raw handle says nothing
+    with pytest.raises(ValueError, match="stream"):
+        b._one_device(types.SimpleNamespace(device_index=1), q=on(0))
+    with pytest.raises(ValueError, match="current device"):
+        b._one_device(object(), q=on(1))
     with pytest.raises(ValueError, match="ws"):
         b._one_device(None, q=on(0), ws=on(1))
     with pytest.raises(ValueError, match="current device"):
