@@ -187,6 +187,7 @@ inline int __builtin_amdgcn_update_dpp(int old, int x, int ctrl, int row_mask, i
   if (ctrl < 0x100) src = (l & ~3) | ((ctrl >> (2 * (l & 3))) & 3);           // quad_perm
   else if (ctrl > 0x110 && ctrl < 0x120) src = in >= (ctrl & 15) ? l - (ctrl & 15) : -1;  // row_shr
   else if (ctrl > 0x120 && ctrl < 0x130) src = row | ((in - (ctrl & 15)) & 15);           // row_ror
+  else if (ctrl >= 0x150 && ctrl < 0x160) src = row | (ctrl & 15);                        // row_newbcast
   else if (ctrl == 0x140) src = row | (15 - in);                               // row_mirror
   else if (ctrl == 0x141) src = row | (in & 8) | (7 - (in & 7));               // row_half_mirror
   else if (ctrl == 0x142) src = row > 0 ? row - 1 : -1;                        // row_bcast:15
