@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
 // cores for 8%. Short rows are bound by the chain of a pair (about 1.4 us), not by bytes. Four waves of a
 // workgroup instead of eight, wave priorities by progress, and workgroups numbered by XCD were within
 // 3% either way.
-constexpr int W = 8;        // waves of a workgroup
+constexpr int kLogW = 3, W = 1 << kLogW;  // waves of a workgroup
 constexpr int kSegment = 1;  // units of a segment beyond its pairs
 // Up to so many pairs of the longest row (half of them unless the waves have several segments each)
 // a wave takes whole segments: what it has more or less than others costs less than states that
@@ -491,6 +491,13 @@ constexpr int kSegment = 1;  // units of a segment beyond its pairs
 // of 100-600 tokens 78 -> 87).
 constexpr int kWhole = 16;
 constexpr int kIdPairs = 32;  // page pairs whose ids a wave holds (one id a lane)
+// Pairs of the longest row times the segments per workgroup, up to which workgroups have segments of
+// their own: four pairs a wave, whose chain is as long as that of a merge over workgroups (one row of
+// 1024 tokens 14.5 us, of 1100 over many workgroups 14.2; Hkv = 8, 64 rows of 100-300 tokens, two segments
+// a workgroup, 14.0 against 17.2, of 100-500 15.6 against 20.6; 32 KV heads, 16 rows of 100-500 15.8 against
+// 20.4). With two pairs or one a segment a wave for each is faster (64 rows of 20-60 8.6 against 9.6).
+constexpr int kOwn = 32;
+static_assert(kOwn <= kIdPairs && W == 8, "the ids fetched ahead are a segment's first");
 
 struct Pair {
   v4u k[2][2], v[2][2];  // [page][half]
@@ -566,9 +573,13 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
   auto fetch_ids = [&](int row, int p) {  // of page pairs p .. p + kIdPairs - 1, one id a lane
     return 2 * p + lane < a.max_pages_per_row ? a.block_table[(size_t)row * a.max_pages_per_row + 2 * p + lane] : 0;
   };
-  // A segment for each workgroup, if none is long: the ids are fetched while the lengths are.
-  const bool few = a.B * a.Hkv <= (int)gridDim.x;
-  const int own_row = few ? min((int)blockIdx.x / a.Hkv, a.B - 1) : -1;
+  // Few segments, none of them long: one for each workgroup, or 2 or 4, each with 8, 4 or 2 waves. The
+  // ids are fetched while the lengths are.
+  const int segments = a.B * a.Hkv, wgs = (int)gridDim.x;
+  const bool few = segments <= 4 * wgs;
+  const int log_per = segments <= wgs ? 0 : segments <= 2 * wgs ? 1 : 2, log_waves = kLogW - log_per;
+  const int own_seg = ((int)blockIdx.x << log_per) + (wave >> log_waves);
+  const int own_row = few ? min(own_seg / a.Hkv, a.B - 1) : -1;
   const int own_ids = few ? fetch_ids(own_row, 0) : 0;
 
   // Lengths -> units before each row (for one KV head), and the longest row's pairs. A length out of
@@ -633,9 +644,10 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     __syncthreads();
   }
 
-  const bool one = few && uniform(longest) <= kIdPairs;  // one segment per workgroup
+  // Segments of a workgroup's own (whole ones of a wave if several would have a pair or two each).
+  const bool own = few && uniform(longest) << log_per <= kOwn && (log_per == 0 || uniform(longest) > 2);
   const int total = uniform(s.pre[a.B]) * a.Hkv;
-  const int nw = one ? a.B * a.Hkv * W : min((int)gridDim.x * W, total);  // waves with work
+  const int nw = own ? segments << log_waves : min(wgs * W, total);  // waves with work
   const int q_units = total / nw, r_units = total - q_units * nw;
   auto begin_of = [&](int w) { return w * q_units + min(w, r_units); };
   auto wave_of = [&](int u) {
@@ -643,19 +655,19 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     return (u < big ? 0 : r_units) + (u < big ? u : u - big) / (u < big ? q_units + 1 : q_units);
   };
   // A wave has whole segments, those that begin in its units.
-  const bool whole = !one && uniform(longest) <= kWhole && uniform(longest) <= max(kWhole / 2, 2 * q_units);
+  const bool whole = !own && uniform(longest) <= kWhole && uniform(longest) <= max(kWhole / 2, 2 * q_units);
   if ((int)blockIdx.x * W >= nw) return;
 
   const int gw = uniform((int)blockIdx.x * W + wave);
   if (gw < nw) {
     // ---- the wave's segments, one after another
     int u, u_end, row, head, off;  // units u .. u_end - 1, from pair `off` of (row, head) on
-    if (one) {
+    if (own) {
       row = own_row;
-      head = (int)blockIdx.x - row * a.Hkv;
-      const int pairs = pairs_of(uniform(s.len[row]));
-      u = off = pairs * wave / W;
-      u_end = pairs > 0 ? pairs * (wave + 1) / W : (wave == 0 ? kSegment : 0);
+      head = own_seg - row * a.Hkv;
+      const int pairs = pairs_of(uniform(s.len[row])), i = wave & ((1 << log_waves) - 1);
+      u = off = pairs * i >> log_waves;
+      u_end = pairs > 0 ? pairs * (i + 1) >> log_waves : (i == 0 ? kSegment : 0);
     } else {
       u = begin_of(gw);
       u_end = begin_of(gw + 1);
@@ -933,7 +945,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       g.states = valid & (next ? (1u << __builtin_ctz(next)) - 1 : 0xFFFFFFFFu) & ~((1u << lane) - 1);
       g.first = g.last = (int)blockIdx.x;
       // the workgroups that hold states of the segment: those of its first to its last pair
-      if (!one && (base < begin_of(blockIdx.x * W) || end > begin_of(blockIdx.x * W + W))) {
+      if (!own && (base < begin_of(blockIdx.x * W) || end > begin_of(blockIdx.x * W + W))) {
         g.first = wave_of(base) / W;
         g.last = wave_of(end - 1) / W;
       }
@@ -989,7 +1001,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
         __builtin_amdgcn_raw_buffer_store_b64(v2u{as_u32(M), as_u32(zero ? -1.0f : L)}, pr, so + (G * D + 2 * h) * 4, 0, kSc1);
     }
   }
-  if (one) return;
+  if (own) return;
 
   // ---- completion count of the (at most two) segments that cross into other workgroups
   __builtin_amdgcn_s_waitcnt(0);

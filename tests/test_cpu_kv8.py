@@ -43,7 +43,8 @@ def test_heads(exe, hq, hkv, fmt):
 @pytest.mark.parametrize("order", SCHEDULES)
 @pytest.mark.parametrize("lens,cus", [([1000], 3), ([1] * 40, 2), ([0, 0, 5, 0], 2), ([2100], 1), ([600, 31, 32, 64, 65, 2], 2),
                                       ([0], 1), ([32] * 9 + [500], 4), ([40, 0, 100, 250, 7, 0, 33, 64] * 3, 2),
-                                      ([500, 30, 512, 0, 60] * 4, 1), ([1100, 0, 900], 3), ([1024, 10], 5)])
+                                      ([500, 30, 512, 0, 60] * 4, 1), ([1100, 0, 900], 3), ([1024, 10], 5),
+                                      ([500, 0, 33], 3), ([250, 1, 0, 100, 256], 3), ([70, 0, 65, 33, 7], 3), ([300, 100, 0], 2)])
 def test_lengths_and_schedules(exe, lens, cus, order):
     attend(exe, Cache(lens, 2, kv8.INT8, seed=5), 8, compute_units=cus, order=order)
 

@@ -53,7 +53,8 @@ def test_heads(g, fmt):
 
 @pytest.mark.parametrize("lens,hkv,hq", [([20011], 8, 32), ([1], 8, 32), ([0], 1, 4), ([5] * 300, 2, 8), ([9000, 3, 0, 1200], 4, 32),
                                          ([33] * 7 + [4000], 1, 1), ([2047, 2048, 2049], 3, 18),
-                                         ([250, 0, 1, 99] * 70, 8, 32), ([500, 512, 0] * 60, 16, 80), ([1024, 1000, 0, 3], 8, 64)])
+                                         ([250, 0, 1, 99] * 70, 8, 32), ([500, 512, 0] * 60, 16, 80), ([1024, 1000, 0, 3], 8, 64),
+                                         ([500, 0, 77, 512] * 15, 8, 32), ([250, 0, 1, 99] * 30, 8, 32)])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_lengths(lens, hkv, hq, fmt):
     d = Device(Cache(lens, hkv, fmt, seed=3), hq)
