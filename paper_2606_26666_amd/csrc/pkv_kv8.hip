@@ -479,9 +479,10 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
 // call has some 13 us that do not depend on its size: the start of the waves and their first ids and
 // pages (5-6), and at the end the slowest wave, the join in the workgroup, and the states' way through
 // memory to the last workgroup and back (6). The vector ALU is busy for 40% of the time, the matrix
-// cores for 8%. Short rows are bound by the chain of a pair (about 1.4 us), not by bytes. Four waves of a
-// workgroup instead of eight, wave priorities by progress, and workgroups numbered by XCD were within
-// 3% either way.
+// cores for 8%. Short rows are bound by the chain of a pair (about 1.4 us), not by bytes. Wave priorities by
+// progress and workgroups numbered by XCD were within 4% either way; four waves of a workgroup instead of
+// eight were slower (64 rows of up to 2048 tokens 55 us against 52), and so were two pairs at a time under
+// one maximum (rows of 16-1024 tokens at G = 8 73 us against 67: every odd pair costs two).
 constexpr int kLogW = 3, W = 1 << kLogW;  // waves of a workgroup
 constexpr int kSegment = 1;  // units of a segment beyond its pairs
 // Up to so many pairs of the longest row (half of them unless the waves have several segments each)
@@ -763,7 +764,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
       enter_ids(lp);
     };
     // K: a load covers eight tokens' whole rows of 128 bytes, the two halves of a row in lanes eight
-    // apart (sort_rows puts them in order): by halves of sixteen rows, 2-4% of the time is lost.
+    // apart (sort_rows puts them in order): by halves of sixteen rows, 1-2% of the time is lost.
     const int k_at = (col & 7) * D + (col >> 3) * 64 + grp * 16, v_at = kKv8CodeBytes + grp * (4 * D) + col * 16;
     const int s_at = kKv8ScaleAt + (col >> 3) * (P * 4) + grp * 16 + (col & 3) * 4;
     auto load = [&](Pair& b) __attribute__((always_inline)) {
