@@ -79,7 +79,8 @@ class Active:
 class Engine:
     """Device state of a slot batch. Prompt K/V is synthetic: a request's pages hold the
     pool's seeded values (no prefill is modelled); each decode step writes the new
-    token's K/V at the row's next position before attending."""
+    token's K/V at the row's next position before attending. `split`, `target_tasks` and
+    `policy` are the planner's, which a cache in 8 bits does without."""
 
     def __init__(self, max_batch: int, max_pages_per_row: int, num_pages: int, hq: int = 32, hkv: int = 8,
                  d: int = 128, split=(16, 64), target_tasks: int = 0, policy: int = 1, mlp: bool = False,
@@ -209,16 +210,16 @@ class Engine:
         if self.format is None:
             raise ValueError("the cache is not in 8 bits")
         torch = self.torch
+        idx = np.arange(self.B)[np.asarray(slots, dtype=np.int64)]
         lens = np.zeros(self.B, dtype=np.int32)  # the calls' rows are the slots: others have no tokens
-        lens[np.asarray(slots, dtype=np.int64)] = self.lens_host[np.asarray(slots, dtype=np.int64)]
+        lens[idx] = self.lens_host[idx]
         offsets = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
         k, v = (torch.empty((int(offsets[-1]), self.hkv, self.d), dtype=torch.float16, device=self.dev) for _ in "kv")
         _b.pkv_kv8_gather(self.cache, self.bt, torch.from_numpy(lens).to(self.dev), k, v, self.bufs.ws, format=self.format,
                           offsets=torch.from_numpy(offsets).to(self.dev))
-        order = np.argsort(np.asarray(slots, dtype=np.int64), kind="stable")
-        if np.array_equal(order, np.arange(len(order))):
+        if np.all(idx[1:] > idx[:-1]):
             return k, v
-        parts = [slice(offsets[s], offsets[s + 1]) for s in slots]  # in the order asked for
+        parts = [slice(offsets[s], offsets[s + 1]) for s in idx]  # in the order asked for, which may repeat one
         return tuple(torch.cat([x[p] for p in parts]) for x in (k, v))
 
 
@@ -310,7 +311,7 @@ def main(argv=None) -> int:
     ap.add_argument("--decode", default="64,256", help="decode length range min,max")
     ap.add_argument("--arrival-gap", type=int, default=0)
     ap.add_argument("--mlp", action="store_true", help="gated-MLP tail (width 11008) after attention")
-    ap.add_argument("--target-tasks", type=int, default=0, help="0: the cost model's rule per step")
+    ap.add_argument("--target-tasks", type=int, default=0, help="0: the cost model's rule per step (fp16 cache)")
     ap.add_argument("--kv", choices=sorted(KV_FORMATS), default="fp16", help="how the cache is held")
     ap.add_argument("--seed", type=int, default=20260623)
     args = ap.parse_args(argv)

@@ -128,3 +128,48 @@ def test_serving_names_its_formats():
     assert KV_FORMATS == {"fp16": None, "int8": pkv.PKV_KV8_INT8, "e4m3": pkv.PKV_KV8_E4M3}
     with pytest.raises(ValueError, match="kv must be"):
         Engine(4, 4, 16, kv="int4")
+
+
+@pytest.mark.parametrize("slots", [[0, 1, 2], [2, 0], [1, 1], [2, 2, 0], [0, 0, 1], [3], [1, 3], [-2, 0], []])
+def test_cached_rows_are_the_slots_asked_for(monkeypatch, slots):
+    """`Engine.cached` and `snapshot` give each slot asked for, in that order, also the same one twice, an
+    empty one and one counted from the end. The read-back is a stand-in that writes 100 * row + position."""
+    import numpy as np
+    from paper_2606_26666_amd import serving
+    lens = np.array([3, 20, 1, 0], dtype=np.int32)
+    tables = np.arange(8, dtype=np.int32).reshape(4, 2)
+
+    def gather(cache, block_table, seq_lens, k, v, ws, *, format, offsets):
+        assert offsets[0] == 0 and offsets[-1] == k.shape[0] and int(seq_lens.sum()) == k.shape[0]
+        for row in range(4):
+            for t in range(int(offsets[row]), int(offsets[row + 1])):
+                pos = int(seq_lens[row]) - (int(offsets[row + 1]) - t)
+                k[t] = 100 * row + pos
+                v[t] = 100 * row + pos + 0.5
+
+    monkeypatch.setattr(serving._b, "pkv_kv8_gather", gather)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    e = object.__new__(serving.Engine)
+    e.torch, e.dev, e.B, e.hq, e.hkv, e.d = torch, torch.device("cpu"), 4, 1, 1, 128
+    e.kv, e.format, e.lens_host, e.bt_host, e.bt = "int8", 0, lens, tables, torch.from_numpy(tables)
+    e.cache, e.bufs = torch.zeros((8, 1, 1)), type("Bufs", (), {"ws": None})
+    e.q = torch.zeros((4, 1, 128), dtype=torch.float16)
+    want = [100 * (s % 4) + p for s in slots for p in range(lens[s])]
+    k, v = e.cached(slots)
+    assert k.shape == v.shape == (len(want), 1, 128)
+    assert k[:, 0, 0].tolist() == want and v[:, 0, 127].tolist() == [x + 0.5 for x in want]
+    _, pool_k, _, bt, n = e.snapshot(slots)
+    assert n.tolist() == [lens[s] for s in slots]
+    for i, s in enumerate(slots):
+        for p in range(n[i]):
+            assert (pool_k[bt[i, p // 16], p % 16] == 100 * (s % 4) + p).all()
+
+
+def test_cached_refuses_a_slot_that_there_is_not():
+    import numpy as np
+    from paper_2606_26666_amd import serving
+    e = object.__new__(serving.Engine)
+    e.torch, e.dev, e.B, e.format, e.lens_host = torch, torch.device("cpu"), 4, 0, np.zeros(4, dtype=np.int32)
+    for slots in ([4], [0, -5]):
+        with pytest.raises(IndexError):
+            e.cached(slots)
