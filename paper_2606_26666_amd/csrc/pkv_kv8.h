@@ -14,8 +14,6 @@ constexpr int kKv8Record = kKv8ScaleAt + 2 * kPageSize * 4;
 constexpr int kKv8MaxG = 8;             // query heads per KV head
 constexpr int kKv8MaxWorkgroups = 512;  // of an attention launch: two state slots each in the workspace
 
-
-
 struct Kv8DecodeArgs {
   const uint16_t* q;
   const uint8_t* cache;

@@ -102,9 +102,9 @@ struct Int8 {
   }
   // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as three
   // balanced base-256 digits of x = round(q * 2^22 / max|q|), x = 65536 d2 + 256 d1 + d0 with d2 in
-  // [-64, 64], d1 and d0 in [-128, 127] (d2's and d1's borders moved up by the digits below them). The sums of digits times codes are exact, and the rounding of
-  // q is 2^-23 of its largest value. First operand: d2 in column h, d1 in column 15 - h; second: d0
-  // in both.
+  // [-64, 64], d1 and d0 in [-128, 127] (d2's and d1's borders moved up by the digits below them). The
+  // sums of digits times codes are exact, and the rounding of q is 2^-23 of its largest value. First
+  // operand: d2 in column h, d1 in column 15 - h; second: d0 in both.
   struct Query {
     v4u b[2][2];  // [first, second][half]
     float unit;   // max|q| * 2^-22 * scale
@@ -910,6 +910,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
     };
 
     // ---- the stream: two pairs are computed, each one's buffer then loads the pair after the other's
+    // (three buffers: one row of 32 K 26 us against 23.5, rows of 16-1024 tokens 72 against 68)
     Pair b0, b1;
     for (bool live = false;;) {
       if (live) attend(b0, cp);
