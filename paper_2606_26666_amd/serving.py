@@ -146,9 +146,9 @@ class Engine:
         self.lens_host[slot] = 0
 
     def step(self, active_slots) -> dict:
-        """Append one token to every active row, attend, run the MLP tail, wait for the
-        device; returns the step's device times (ms: attention, whole step) from events
-        on the current stream."""
+        """Append one token to every active row, attend over all admitted ones, run the MLP
+        tail, wait for the device; returns the step's device times (ms: attention, whole
+        step) from events on the current stream."""
         torch = self.torch
         ev = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
         idx = np.asarray(active_slots, dtype=np.int64)
@@ -157,7 +157,7 @@ class Engine:
         self.lens_host[idx] += 1
         ev[0].record()
         if idx.size and self.format is not None:
-            k, v = self._new_tokens(self.B)      # a token for every slot; free ones are skipped
+            k, v = self._new_tokens(self.B)      # a token for every slot; those not stepped are skipped
             self.q.normal_(generator=self.gen)
             self.q.mul_(1.0 / np.sqrt(self.d))
         elif idx.size:
@@ -177,7 +177,10 @@ class Engine:
                                b.num_tasks, 1.0, self.out, b.ws)
         else:
             if idx.size:
-                _b.pkv_kv8_append(k, v, self.cache, self.bt, self.lens, b.ws, format=self.format)
+                grown = np.zeros_like(self.lens_host)   # length 0: no token is written
+                grown[idx] = self.lens_host[idx]
+                lens = self.lens if np.array_equal(grown, self.lens_host) else torch.from_numpy(grown).to(self.dev)
+                _b.pkv_kv8_append(k, v, self.cache, self.bt, lens, b.ws, format=self.format)
             _b.pkv_kv8_decode(self.q, self.cache, self.bt, self.lens, 1.0, self.out, b.ws, format=self.format)
         ev[1].record()
         if self.mlp is not None and idx.size:
