@@ -353,7 +353,7 @@ int pkv_stream_read_pages(const uint16_t* k_cache, const uint16_t* v_cache, int3
  *     PKV_KV8_INT8  scale = m / 127, code = x * 127 / m rounded to the nearest integer (ties to even)
  *     PKV_KV8_E4M3  scale = m / 448, code = x * 448 / m rounded to the nearest e4m3 (ties to even)
  * (the codes are exactly those of real arithmetic; the scale is m / 127 or m / 448 rounded to fp32).
- * m = 0 gives scale 0. A vector with an infinity or NaN gets scale NaN and codes 0, so all its values
+ * m = 0 gives scale 0 and codes 0. A vector with an infinity or NaN gets scale NaN and codes 0, so all its values
  * read back as NaN, and attention over it gives NaN.
  *
  * Shared by the three calls: d = 128 (else PKV_ERR_UNSUPPORTED); block_table int32 [B,

@@ -308,7 +308,7 @@ __device__ __forceinline__ v2u quantise(v4u raw, float& scale) {
   const h8v x = __builtin_bit_cast(h8v, raw);
   float y[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = finite ? round21((float)x[j] * inv) : 0.0f;
+  for (int j = 0; j < 8; ++j) y[j] = inv > 0.0f ? round21((float)x[j] * inv) : 0.0f;  // (also a vector of -0: codes 0)
   return v2u{F::code4(y[0], y[1], y[2], y[3]), F::code4(y[4], y[5], y[6], y[7])};
 }
 

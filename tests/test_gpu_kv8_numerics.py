@@ -1,0 +1,25 @@
+"""Numerics of the 8-bit cache's kernels at their borders, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_26666_amd as pkv
+from oracle import kv8
+from tests.cpu_kv8 import Cache
+from tests.test_cpu_kv8_numerics import FORMATS, signed_zeros
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to("cuda")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_zeros_of_both_signs(fmt):
+    x = signed_zeros()
+    for c, offs in ((Cache([8], 2, fmt, filled=False), [0, 8]), (Cache([3] * 8, 2, fmt, filled=False), None)):
+        pool, ws = dev(c.pool), pkv.Kv8Buffers(c.B, 2, 2, 128, "cuda").ws
+        pkv.pkv_kv8_append(dev(x), dev(x[::-1]), pool, dev(c.bt), dev(c.lens), ws, format=fmt,
+                           offsets=None if offs is None else dev(np.array(offs, dtype=np.int32)))
+        assert np.array_equal(pool.cpu().numpy(), kv8.ref_append(c.pool, x, x[::-1], c.bt, c.lens, fmt, offs))
