@@ -50,6 +50,20 @@ __device__ __forceinline__ float across_rows(float x, F f) {
   return f(as_f32((unsigned)t[0]), as_f32((unsigned)t[1]));
 }
 
+// Eight query values as bf16 high halves in a head's column h and low halves in column 15 - h (exact: fp16
+// has 11 bits). `there`: the column has a head.
+__device__ __forceinline__ b8v bf16_halves(v4u raw, bool there, int col) {
+  const h8v y = __builtin_bit_cast(h8v, raw);
+  b8v b;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float f = there ? (float)y[e] : 0.0f;
+    const __bf16 hi = (__bf16)f;
+    b[e] = col < 8 ? hi : (__bf16)(f - (float)hi);
+  }
+  return b;
+}
+
 template <typename F>
 __device__ __forceinline__ b8v load8(unsigned lo, unsigned hi) {
   const v2u a = F::load4(lo), b = F::load4(hi);
@@ -100,15 +114,20 @@ struct Int8 {
     const float c = (float)(signed char)((w >> 16) & 255u), d = (float)(signed char)(w >> 24);
     return v2u{__builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302u), __builtin_amdgcn_perm(as_u32(d), as_u32(c), 0x07060302u)};
   }
-  // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as three
-  // balanced base-256 digits of x = round(q * 2^22 / max|q|), x = 65536 d2 + 256 d1 + d0 with d2 in
-  // [-64, 64], d1 and d0 in [-128, 127] (d2's and d1's borders moved up by the digits below them). The
-  // sums of digits times codes are exact, and the rounding of q is 2^-23 of its largest value. First
-  // operand: d2 in column h, d1 in column 15 - h; second: d0 in both.
+  // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as four
+  // balanced base-256 digits of x = q * 2^k, x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 with d3 in [-64, 64], the
+  // others in [-128, 127] (a digit's borders moved up by the digits below it). k is the largest up to 24
+  // with max|q| * 2^k <= 2^30. Where every x of the wave's heads is an integer (below 64 every fp16 is;
+  // above, one without bits below 2^-30 of its head's largest value, taken up to a power of two), the
+  // sums of digits times codes are exact, and the sum of each pair of digits is rounded once, to fp32.
+  // Else the query goes in as bf16 halves and K is converted, as in E4m3, so that no bit of a small value
+  // is lost beside a large one.
+  // First operand: d3 in column h, d2 in column 15 - h; second: d1 and d0.
   struct Query {
-    v4u b[2][2];  // [first, second][half]
-    float unit;   // max|q| * 2^-22 * scale
-    int shift;    // of the own column's sum: 8 for d2, 0 for d1
+    v4u b[4];     // digits: [first, second][half]; else a quarter's bf16 each
+    float unit;   // 2^-k * scale, or the scale
+    int shift;    // of the own column's sum: 8 for d3 and d1, 0 for d2 and d0
+    bool digits;
     __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
       unsigned top = 0;
 #pragma unroll
@@ -116,41 +135,72 @@ struct Int8 {
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = max(top, max(raw[j][e] & 0x7FFFu, (raw[j][e] >> 16) & 0x7FFFu));
       top = as_u32(across_rows(as_f32(top), [](float y, float z) { return as_f32(max(as_u32(y), as_u32(z))); }));
-      const float most = there ? (float)__builtin_bit_cast(_Float16, (uint16_t)top) : 0.0f;
-      unit = top < 0x7C00u ? most * 0x1p-22f * scale : __builtin_nanf("");
-      const float inv = most > 0.0f && top < 0x7C00u ? 0x1p22f / most : 0.0f;
+      const bool finite = there && top < 0x7C00u;
+      const int k = min(24, 44 - (int)(top >> 10));  // |q| < 2^(exponent bits - 14)
+      const float up = finite ? as_f32((unsigned)(127 + k) << 23) : 0.0f;
       shift = col < 8 ? 8 : 0;
-      // 1.5 * 2^23 + q * inv, rounded once, has x in its low bits, 0x4B400000 above. A byte of x + bias
-      // is a digit: d2 = (x + 2^15 + 2^7) >> 16, d1 the low byte of (x + 2^7) >> 8, d0 that of x.
-      const unsigned bias = (col < 8 ? 0x8080u : 0x80u) - 0x400000u;
-      const unsigned low = col < 8 ? 0x0C0C0602u : 0x0C0C0501u;  // bytes 2 or 1 of a pair
+      digits = true;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(finite && k < 24) != 0, 0)) {
+        bool whole = true;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const h8v y = __builtin_bit_cast(h8v, raw[j]);
-        unsigned x[8];
+        for (int j = 0; j < 4; ++j) {
+          const h8v y = __builtin_bit_cast(h8v, raw[j]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = inv > 0.0f ? as_u32(__builtin_fmaf((float)y[e], inv, 12582912.0f)) : 0x4B400000u;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const unsigned* z = x + 4 * i;
-          b[0][j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias, z[0] + bias, low) |
-                                          __builtin_amdgcn_perm(z[3] + bias, z[2] + bias, low) << 16;
-          b[1][j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1], z[0], 0x0C0C0400u) | __builtin_amdgcn_perm(z[3], z[2], 0x04000C0Cu);
+          for (int e = 0; e < 8; ++e) {
+            const float x = finite ? (float)y[e] * up : 0.0f;
+            whole = whole && x == __builtin_truncf(x);
+          }
         }
+        digits = __builtin_amdgcn_ballot_w64(!whole) == 0;
+      }
+      if (__builtin_expect(digits, 1)) {
+        unit = top < 0x7C00u ? as_f32((unsigned)(127 - k) << 23) * scale : __builtin_nanf("");
+        // A byte of x + bias is a digit: d3 that of 2^24 of x + 2^23 + 2^15 + 2^7, and so on.
+        const unsigned bias1 = col < 8 ? 0x808080u : 0x8080u, bias0 = col < 8 ? 0x80u : 0u;
+        const unsigned at1 = col < 8 ? 0x0C0C0703u : 0x0C0C0602u, at0 = col < 8 ? 0x0C0C0501u : 0x0C0C0400u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const h8v y = __builtin_bit_cast(h8v, raw[j]);
+          unsigned x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = (unsigned)(int)(finite ? (float)y[e] * up : 0.0f);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const unsigned* z = x + 4 * i;
+            b[j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias1, z[0] + bias1, at1) |
+                                         __builtin_amdgcn_perm(z[3] + bias1, z[2] + bias1, at1) << 16;
+            b[2 + (j >> 1)][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias0, z[0] + bias0, at0) |
+                                               __builtin_amdgcn_perm(z[3] + bias0, z[2] + bias0, at0) << 16;
+          }
+        }
+      } else {
+        unit = scale;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(v4u, bf16_halves(raw[j], there, col));
       }
     }
     __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
+      v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (__builtin_expect(!digits, 0)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<Int8>(k[j >> 1][2 * (j & 1)], k[j >> 1][2 * (j & 1) + 1]),
+                                                      __builtin_bit_cast(b8v, b[j]), x, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (x[i] + mirror16(x[i])) * (ks[i] * unit);
+        return x;
+      }
       v4i c = {0, 0, 0, 0}, c0 = {0, 0, 0, 0};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[0][half]), c, 0, 0, 0);
-        c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[1][half]), c0, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[half]), c, 0, 0, 0);
+        c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[2 + half]), c0, 0, 0, 0);
       }
-      v4f x;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = (c[i] << shift) + (dpp<0x140>(c[i]) << (8 - shift));
-        x[i] = __builtin_fmaf((float)t, 256.0f, (float)c0[i]) * (ks[i] * unit);
+        const int t0 = (c0[i] << shift) + (dpp<0x140>(c0[i]) << (8 - shift));
+        x[i] = __builtin_fmaf((float)t, 65536.0f, (float)t0) * (ks[i] * unit);
       }
       return x;
     }
@@ -171,23 +221,14 @@ struct E4m3 {
     return v2u{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
   }
-  // Q.K in bf16: K exactly, a query value as its bf16 high half in column h and low half in column
-  // 15 - h (exact: fp16 has 11 bits); the two columns' sums are added.
+  // Q.K in bf16: K exactly, a query's halves (exact); the two columns' sums are added.
   struct Query {
     b8v b[4];
     float unit;
     __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
       unit = scale;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const h8v y = __builtin_bit_cast(h8v, raw[j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float f = there ? (float)y[e] : 0.0f;
-          const __bf16 hi = (__bf16)f;
-          b[j][e] = col < 8 ? hi : (__bf16)(f - (float)hi);
-        }
-      }
+      for (int j = 0; j < 4; ++j) b[j] = bf16_halves(raw[j], there, col);
     }
     __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
       v4f x = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -32,6 +32,51 @@ def assert_decode(out, q, pool, bt, lens, fmt, sm_scale, what=""):
     assert np.all(err <= tol), (what, float((err / tol).max()), float(np.nanmax(err)))
 
 
+def fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores):
+    """(reference, bound) [B, Hq, 128] for rows of at most 32 tokens, whose weights are formed under one
+    maximum, with no factor that real errors cannot reach. With S = |scale| sum|q k| of a token:
+    - a score s: the scale to fp32 and times log2(e), that times the query's unit and the K scale, and the sum
+      times that: five roundings, 2^-24 each. The sum itself: in integers (exact_scores) two sums of magnitude S
+      and 2 S at most are rounded, 2^-24 each; in bf16 each of 129 additions is off by at most 2^-23 of S.
+    - a weight, relatively: the error of s; s - max rounded, 2^-24 of it; exp2 2^-23.
+    - a weight's error d moves the output by p d |v - o| (p: the weight over the weights' sum, o: the output).
+    - weight times V scale 2^-24 and its parts 2^-24; a dim's sum has three parts of n products, each addition off by
+      at most 2^-23 of mean|v|; the sum of weights n + 4 roundings, its reciprocal and product 2^-22, of o.
+    - the output's rounding: 2^-11 of the value, 2^-25 where it is subnormal."""
+    ref = kv8.ref_decode8(q, pool, bt, lens, fmt, sm_scale)
+    tol = np.abs(ref) * 2.0 ** -11 + 2.0 ** -25
+    hq, hkv = q.shape[1], pool.shape[1]
+    for i, n in enumerate(np.asarray(lens).tolist()):
+        assert n <= 32
+        if n == 0:
+            continue
+        K, V = kv8.stored(pool, bt[i], n, fmt)
+        for h in range(hq):
+            k, v, x = K[:, h // (hq // hkv)], V[:, h // (hq // hkv)], q[i, h].astype(np.float64)
+            s, size = sm_scale * (k @ x), abs(sm_scale) * (np.abs(k) @ np.abs(x))
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            d = 2.0 ** -24 * (5 * np.abs(s) + (3 if exact_scores else 2 * 129) * size + np.abs(s - s.max())) + 2.0 ** -23
+            tol[i, h] += (p * d) @ np.abs(v - ref[i, h]) + (p @ np.abs(v)) * (2.0 ** -23 + 3 * n * 2.0 ** -23)
+            tol[i, h] += np.abs(ref[i, h]) * ((n + 4) * 2.0 ** -24 + 2.0 ** -22)
+    return ref, tol
+
+
+def assert_fine(out, q, pool, bt, lens, fmt, sm_scale, exact_scores):
+    ref, tol = fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores)
+    err = np.abs(np.asarray(out, dtype=np.float64) - ref)
+    assert np.all(err <= tol), (float((err / tol).max()), float(np.nanmax(err)))
+
+
+def outlier_queries(cache, hq, large, small, seed=3):
+    """Queries with one large channel whose K codes are all 0: the scores are those of the small ones."""
+    r = np.random.default_rng(seed)
+    kv8.views(cache.pool)[0][..., 5] = 0
+    q = (r.standard_normal((cache.B, hq, 128)) * small).astype(np.float16)
+    q[..., 5] = large
+    return q
+
+
 def gathered(pool, bt_row, begin, end, fmt):
     """The row's tokens [begin, end) as the read-back gives them: fp16 of the fp32 product."""
     k, v, ks, vs = kv8.views(pool[np.asarray(bt_row[begin // 16:-(-end // 16)], dtype=np.int64)])

@@ -7,6 +7,7 @@ from oracle import kv8
 from tests import cpu_kv8
 from tests.cpu_cases import compiler
 from tests.cpu_kv8 import Cache, call
+from tests.kv8_cases import assert_fine, outlier_queries
 
 FORMATS = [kv8.INT8, kv8.E4M3]
 
@@ -39,3 +40,29 @@ def test_zeros_of_both_signs(exe, fmt, offsets):
                                 offsets=None if offsets is None else np.array(offsets))
     assert (st, bits) == (0, 0)
     assert np.array_equal(pool, kv8.ref_append(c.pool, x, x[::-1], c.bt, c.lens, fmt, offsets))
+
+
+# The large channel, the size of the others (2: multiples of 1/64) and of K, and whether the int8 scores are
+# sums of integers: 30 bits from the large channel down reach to 2^-14 (60000), 2^-16 (16000), 2^-21 (300) or, below
+# 64, to the last bit of fp16.
+OUTLIERS = [(60000, 2.0, 1, True), (16000, 2.0, 1, True), (40, 1.0, 1, True), (60000, 0.01, 100, False), (300, 1e-4, 2000, False),
+            (6e-5, 3e-7, 30000, True), (60000, 0, 1, True)]
+
+
+def outlier_case(fmt, large, small, k_size):
+    c = Cache([31, 1, 0, 32, 17], 2, fmt, seed=14)
+    q = outlier_queries(c, 8, large, small)
+    kv8.views(c.pool)[2][:] *= k_size
+    if small == 2.0:  # no values that end below the unit of the digits
+        q[..., 6:] = np.rint(q[..., 6:].astype(np.float64) * 64) / 64
+        q[..., :5] = np.rint(q[..., :5].astype(np.float64) * 64) / 64
+    return c, q
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("large,small,k_size,digits", OUTLIERS)
+def test_one_large_query_channel(exe, fmt, large, small, k_size, digits):
+    c, q = outlier_case(fmt, large, small, k_size)
+    (st, bits, _, out), = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)
+    assert (st, bits) == (0, 0)
+    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)

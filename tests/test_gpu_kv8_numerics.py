@@ -6,7 +6,8 @@ import torch
 import paper_2606_26666_amd as pkv
 from oracle import kv8
 from tests.cpu_kv8 import Cache
-from tests.test_cpu_kv8_numerics import FORMATS, signed_zeros
+from tests.kv8_cases import assert_fine
+from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,20 @@ def test_zeros_of_both_signs(fmt):
         pkv.pkv_kv8_append(dev(x), dev(x[::-1]), pool, dev(c.bt), dev(c.lens), ws, format=fmt,
                            offsets=None if offs is None else dev(np.array(offs, dtype=np.int32)))
         assert np.array_equal(pool.cpu().numpy(), kv8.ref_append(c.pool, x, x[::-1], c.bt, c.lens, fmt, offs))
+
+
+def attend(c, q, hq):
+    """An attention call over a Cache's arrays: its output on the host."""
+    bufs = pkv.Kv8Buffers(c.B, hq, c.hkv, 128, "cuda")
+    bufs.partial_region().fill_(0xFF)
+    out = torch.full((c.B, hq, 128), float("nan"), dtype=torch.float16, device="cuda")
+    pkv.pkv_kv8_decode(dev(q), dev(c.pool), dev(c.bt), dev(c.lens), 0.09, out, bufs.ws, format=c.fmt)
+    assert pkv.pkv_check_device_status(bufs.ws) == 0
+    return out.cpu().numpy()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("large,small,k_size,digits", OUTLIERS)
+def test_one_large_query_channel(fmt, large, small, k_size, digits):
+    c, q = outlier_case(fmt, large, small, k_size)
+    assert_fine(attend(c, q, 8), q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)
