@@ -119,14 +119,13 @@ struct Int8 {
   // others in [-128, 127] (a digit's borders moved up by the digits below it). k is the largest up to 24
   // with max|q| * 2^k <= 2^30. Where every x of the wave's heads is an integer (below 64 every fp16 is;
   // above, one without bits below 2^-30 of its head's largest value, taken up to a power of two), the
-  // sums of digits times codes are exact, and the sum of each pair of digits is rounded once, to fp32.
+  // sums of digits times codes are exact, and two of them joined (d3 and d1, d2 and d0) rounded to fp32.
   // Else the query goes in as bf16 halves and K is converted, as in E4m3, so that no bit of a small value
   // is lost beside a large one.
   // First operand: d3 in column h, d2 in column 15 - h; second: d1 and d0.
   struct Query {
     v4u b[4];     // digits: [first, second][half]; else a quarter's bf16 each
-    float unit;   // 2^-k * scale, or the scale
-    int shift;    // of the own column's sum: 8 for d3 and d1, 0 for d2 and d0
+    float unit;   // 2^-k * scale, and 2^8 in the columns of d3 and d1; or the scale
     bool digits;
     __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
       unsigned top = 0;
@@ -138,7 +137,6 @@ struct Int8 {
       const bool finite = there && top < 0x7C00u;
       const int k = min(24, 44 - (int)(top >> 10));  // |q| < 2^(exponent bits - 14)
       const float up = finite ? as_f32((unsigned)(127 + k) << 23) : 0.0f;
-      shift = col < 8 ? 8 : 0;
       digits = true;
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(finite && k < 24) != 0, 0)) {
         bool whole = true;
@@ -154,7 +152,7 @@ struct Int8 {
         digits = __builtin_amdgcn_ballot_w64(!whole) == 0;
       }
       if (__builtin_expect(digits, 1)) {
-        unit = top < 0x7C00u ? as_f32((unsigned)(127 - k) << 23) * scale : __builtin_nanf("");
+        unit = top < 0x7C00u ? as_f32((unsigned)((col < 8 ? 135 : 127) - k) << 23) * scale : __builtin_nanf("");
         // A byte of x + bias is a digit: d3 that of 2^24 of x + 2^23 + 2^15 + 2^7, and so on.
         const unsigned bias1 = col < 8 ? 0x808080u : 0x8080u, bias0 = col < 8 ? 0x80u : 0u;
         const unsigned at1 = col < 8 ? 0x0C0C0703u : 0x0C0C0602u, at0 = col < 8 ? 0x0C0C0501u : 0x0C0C0400u;
@@ -198,9 +196,8 @@ struct Int8 {
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int t = (c[i] << shift) + (dpp<0x140>(c[i]) << (8 - shift));
-        const int t0 = (c0[i] << shift) + (dpp<0x140>(c0[i]) << (8 - shift));
-        x[i] = __builtin_fmaf((float)t, 65536.0f, (float)t0) * (ks[i] * unit);
+        x[i] = __builtin_fmaf((float)c[i], 65536.0f, (float)c0[i]) * (ks[i] * unit);
+        x[i] += mirror16(x[i]);
       }
       return x;
     }
