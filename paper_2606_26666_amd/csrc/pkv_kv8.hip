@@ -120,12 +120,16 @@ struct Int8 {
   // with max|q| * 2^k <= 2^30. Where every x of the wave's heads is an integer (below 64 every fp16 is;
   // above, one without bits below 2^-30 of its head's largest value, taken up to a power of two), the
   // sums of digits times codes are exact, and two of them joined (d3 and d1, d2 and d0) rounded to fp32.
+  // A head's columns have to hold the same score to the last bit, since they hold parts of the same weight: they
+  // are added before the scales come in, so that no product can be fused into the sum of one column and
+  // not into the other's.
   // Else the query goes in as bf16 halves and K is converted, as in E4m3, so that no bit of a small value
   // is lost beside a large one.
   // First operand: d3 in column h, d2 in column 15 - h; second: d1 and d0.
   struct Query {
     v4u b[4];     // digits: [first, second][half]; else a quarter's bf16 each
-    float unit;   // 2^-k * scale, and 2^8 in the columns of d3 and d1; or the scale
+    float unit;   // 2^-k * scale, or the scale
+    float up;     // 2^8 in the columns of d3 and d1, 1 in the others
     bool digits;
     __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
       unsigned top = 0;
@@ -136,8 +140,9 @@ struct Int8 {
       top = as_u32(across_rows(as_f32(top), [](float y, float z) { return as_f32(max(as_u32(y), as_u32(z))); }));
       const bool finite = there && top < 0x7C00u;
       const int k = min(24, 44 - (int)(top >> 10));  // |q| < 2^(exponent bits - 14)
-      const float up = finite ? as_f32((unsigned)(127 + k) << 23) : 0.0f;
+      const float raise = finite ? as_f32((unsigned)(127 + k) << 23) : 0.0f;
       digits = true;
+      up = col < 8 ? 256.0f : 1.0f;
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(finite && k < 24) != 0, 0)) {
         bool whole = true;
 #pragma unroll
@@ -145,14 +150,14 @@ struct Int8 {
           const h8v y = __builtin_bit_cast(h8v, raw[j]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float x = finite ? (float)y[e] * up : 0.0f;
+            const float x = finite ? (float)y[e] * raise : 0.0f;
             whole = whole && x == __builtin_truncf(x);
           }
         }
         digits = __builtin_amdgcn_ballot_w64(!whole) == 0;
       }
       if (__builtin_expect(digits, 1)) {
-        unit = top < 0x7C00u ? as_f32((unsigned)((col < 8 ? 135 : 127) - k) << 23) * scale : __builtin_nanf("");
+        unit = top < 0x7C00u ? as_f32((unsigned)(127 - k) << 23) * scale : __builtin_nanf("");
         // A byte of x + bias is a digit: d3 that of 2^24 of x + 2^23 + 2^15 + 2^7, and so on.
         const unsigned bias1 = col < 8 ? 0x808080u : 0x8080u, bias0 = col < 8 ? 0x80u : 0u;
         const unsigned at1 = col < 8 ? 0x0C0C0703u : 0x0C0C0602u, at0 = col < 8 ? 0x0C0C0501u : 0x0C0C0400u;
@@ -161,7 +166,7 @@ struct Int8 {
           const h8v y = __builtin_bit_cast(h8v, raw[j]);
           unsigned x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = (unsigned)(int)(finite ? (float)y[e] * up : 0.0f);
+          for (int e = 0; e < 8; ++e) x[e] = (unsigned)(int)(finite ? (float)y[e] * raise : 0.0f);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const unsigned* z = x + 4 * i;
@@ -196,8 +201,8 @@ struct Int8 {
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = __builtin_fmaf((float)c[i], 65536.0f, (float)c0[i]) * (ks[i] * unit);
-        x[i] += mirror16(x[i]);
+        const float y = __builtin_fmaf((float)c[i], 65536.0f * up, (float)c0[i] * up);
+        x[i] = (y + mirror16(y)) * (ks[i] * unit);
       }
       return x;
     }

@@ -38,8 +38,9 @@ def fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores):
     - a score s: the scale to fp32 and times log2(e), that times the query's unit and the K scale, and the sum
       times that, and the sum of its two halves: five roundings, 2^-24 each. The halves themselves: in integers
       (exact_scores) the query x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 is taken as d3, d1 and d2, d0; each half's sum is
-      rounded when it is joined and when it is scaled, and |2^24 d3 + 2^8 d1| + |2^16 d2 + d0| <= 3.01 |x| (the second
-      sum is at most 2^23 + 2^7, and d3 = 0 unless |x| >= 2^23 - 2^15 - 2^7): 6.1 S of 2^-24. In bf16 each of 129 additions is off by at most 2^-23 of S.
+      rounded once, and |2^24 d3 + 2^8 d1| + |2^16 d2 + d0| <= 3.01 |x| (the second sum is at most 2^23 + 2^7, and
+      d3 = 0 unless |x| >= 2^23 - 2^15 - 2^7): 3.1 S of 2^-24. In bf16 each of 129
+      additions is off by at most 2^-23 of S.
     - a weight, relatively: the error of s; s - max rounded, 2^-24 of it; exp2 2^-23.
     - a weight's error d moves the output by p d |v - o| (p: the weight over the weights' sum, o: the output).
     - weight times V scale 2^-24 and its parts 2^-24; a dim's sum has three parts of n products, each addition off by
@@ -58,7 +59,7 @@ def fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores):
             s, size = sm_scale * (k @ x), abs(sm_scale) * (np.abs(k) @ np.abs(x))
             p = np.exp(s - s.max())
             p /= p.sum()
-            d = 2.0 ** -24 * (5 * np.abs(s) + (6.1 if exact_scores else 2 * 129) * size + np.abs(s - s.max())) + 2.0 ** -23
+            d = 2.0 ** -24 * (5 * np.abs(s) + (3.1 if exact_scores else 2 * 129) * size + np.abs(s - s.max())) + 2.0 ** -23
             tol[i, h] += (p * d) @ np.abs(v - ref[i, h]) + (p @ np.abs(v)) * (2.0 ** -23 + 3 * n * 2.0 ** -23)
             tol[i, h] += np.abs(ref[i, h]) * ((n + 4) * 2.0 ** -24 + 2.0 ** -22)
     return ref, tol

@@ -6,7 +6,7 @@ import torch
 import paper_2606_26666_amd as pkv
 from oracle import kv8
 from tests.cpu_kv8 import Cache
-from tests.kv8_cases import assert_fine
+from tests.kv8_cases import assert_decode, assert_fine
 from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +41,13 @@ def attend(c, q, hq):
 def test_one_large_query_channel(fmt, large, small, k_size, digits):
     c, q = outlier_case(fmt, large, small, k_size)
     assert_fine(attend(c, q, 8), q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq", [8, 16])
+def test_columns_of_a_head_agree(fmt, hq):
+    """A weight's parts lie in several columns, each with a score of its own: where two scores differ in the last
+    bit, one weight in some 2^15 is off by 2^-8. Here there are 5 weights for each of 4096 rows' heads."""
+    c = Cache([5] * 4096, 2, fmt, seed=3)
+    q = np.random.default_rng(8).standard_normal((4096, hq, 128)).astype(np.float16)
+    assert_decode(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09)
