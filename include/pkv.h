@@ -413,8 +413,8 @@ int pkv_kv8_gather(const void* cache, int32_t num_pages, const int32_t* block_ta
  * Hq / Hkv from 1 to 8 and B <= 4096, else PKV_ERR_UNSUPPORTED; also when B * Hkv *
  * (max_pages_per_row / 2 + 2) passes 2^31 - 1. Rows whose length is out of range (PKV_DEVERR_SEQ_LEN)
  * or that name a page outside the pool (PKV_DEVERR_PAGE_ID) are written as zeros. Scores (formed
- * from the query's and the codes' exact products), softmax statistics and sums are fp32; the weights enter P.V as two bf16 halves (16 bits). Results do not
- * depend on anything but the inputs and the device's compute units. */
+ * from the query's and the codes' exact products), softmax statistics, weights and sums are fp32.
+ * Results do not depend on anything but the inputs and the device's compute units. */
 int pkv_kv8_decode(const uint16_t* q, int64_t q_stride, const void* cache, int32_t num_pages,
                    const int32_t* block_table, int32_t max_pages_per_row, const int32_t* seq_lens, int32_t B,
                    int32_t Hq, int32_t Hkv, int32_t d, int32_t format, float sm_scale, uint16_t* out, void* ws,

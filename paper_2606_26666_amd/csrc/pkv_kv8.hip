@@ -513,9 +513,9 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
 // holding tokens 4 grp .. 4 grp + 3 of its column's head: the layout that the second product's B
 // operand has, so the weights go from one product to the next without leaving their lanes.
 // P V: A = V^T, 16 dims by the pair's 32 tokens, B = the weights (times the tokens' V scales)
-// as bf16 high halves in column h and low halves in column 15 - h. The record's V layout gives each
-// lane its four tokens of eight dims as whole dwords, and K is token-major: codes go from HBM into
-// registers and from there into the matrix cores, without LDS.
+// in bf16 parts, the first in column h, the second in column 15 - h, the last in a product of its
+// own. The record's V layout gives each lane its four tokens of eight dims as whole dwords, and K is
+// token-major: codes go from HBM into registers and from there into the matrix cores, without LDS.
 //
 // What bounds it: reading the records. 32 rows of up to 32 K tokens (928 MB) take 151 us, 6.2 TB/s of
 // the 6.9 that a large read reaches; without any arithmetic the same loads take 149. Beyond the read a
@@ -855,7 +855,7 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
 #pragma unroll
       for (int t = 0; t < 8; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] += mirror16(acc[t][i]);  // the low halves' sums join
+        for (int i = 0; i < 4; ++i) acc[t][i] += mirror16(acc[t][i]);  // the second parts' sums join
       const float sum = across_rows(l, [](float x, float y) { return x + y; });
       const bool begins = cs.p0 == 0, ends = cs.p1 == cs.pairs;
       if (wrong && lane == 0) atomicOr(a.err, (unsigned)PKV_DEVERR_PAGE_ID);
@@ -932,22 +932,34 @@ __global__ __launch_bounds__(W * 64, 2) void kv8_decode_kernel(Kv8DecodeArgs a) 
         for (int t = 0; t < 8; ++t) acc[t] *= v4f{c, c, c, c};
         m = top;
       }
-      // A weight times its token's V scale as two bf16 halves: 16 bits, 2^-16 of it, where the output
-      // keeps 11. bf16 has fp32's range, so no scale is too small or large for it; sums stay fp32.
-      b8v w;
+      // A weight times its token's V scale in three bf16 parts of eight bits each, from the top down: all 24 bits
+      // of it, so values that cancel in the sum cost no more than in fp32. bf16 has fp32's range, so no
+      // scale is too small or large for it. The last part, for which the columns have no place, is a product
+      // of its own (eight more matrix instructions a pair: 64 rows of 128-4096 tokens 52.7 us against 52.5
+      // without it; with up to four heads in columns left over it is no faster, at 19 registers more).
+      v4u w, w0;
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = ex2(x[pg][i] - m);
-          l += e;
-          const float f = e * vs[pg][i];
-          const __bf16 hi = (__bf16)f;
-          w[4 * pg + i] = col < 8 ? hi : (__bf16)(f - (float)hi);
+        for (int i = 0; i < 4; i += 2) {
+          float own[2], low[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float e = ex2(x[pg][i + j] - m);
+            l += e;
+            const float f = e * vs[pg][i + j];
+            const float rest = f - as_f32(as_u32(f) & 0xFFFF0000u), last = rest - as_f32(as_u32(rest) & 0xFFFF0000u);
+            own[j] = col < 8 ? f : rest;
+            low[j] = col < 8 ? last : 0.0f;
+          }
+          w[2 * pg + i / 2] = __builtin_amdgcn_perm(as_u32(own[1]), as_u32(own[0]), 0x07060302u);  // upper halves
+          w0[2 * pg + i / 2] = __builtin_amdgcn_perm(as_u32(low[1]), as_u32(low[0]), 0x07060302u);
         }
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<F>(b.v[0][t >> 2][t & 3], b.v[1][t >> 2][t & 3]), w, acc[t], 0, 0, 0);
+        const b8v v = load8<F>(b.v[0][t >> 2][t & 3], b.v[1][t >> 2][t & 3]);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(b8v, w), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(b8v, w0), acc[t], 0, 0, 0);
         if (t & 1) __builtin_amdgcn_sched_barrier(0);  // the conversions of a few tiles at a time: else they spill
       }
     };

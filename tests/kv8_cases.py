@@ -80,6 +80,17 @@ def outlier_queries(cache, hq, large, small, seed=3):
     return q
 
 
+def opposed_values(rows, hq, fmt, seed=6):
+    """Rows of two tokens with nearly equal scores and opposed V: outputs are a small part of the values."""
+    from tests.cpu_kv8 import Cache
+    c, r = Cache([2] * rows, 2, fmt, seed=seed), np.random.default_rng(seed)
+    _, v, _, vs = kv8.views(c.pool)
+    first = c.bt[:, 0]
+    v[first, :, 0, :, 1] = -v[first, :, 0, :, 0].view(np.int8).astype(np.int16) if fmt == kv8.INT8 else v[first, :, 0, :, 0] ^ 128
+    vs[first, :, 1] = vs[first, :, 0]
+    return c, (r.standard_normal((rows, hq, 128)) * 0.002).astype(np.float16)
+
+
 def gathered(pool, bt_row, begin, end, fmt):
     """The row's tokens [begin, end) as the read-back gives them: fp16 of the fp32 product."""
     k, v, ks, vs = kv8.views(pool[np.asarray(bt_row[begin // 16:-(-end // 16)], dtype=np.int64)])

@@ -7,7 +7,7 @@ from oracle import kv8
 from tests import cpu_kv8
 from tests.cpu_cases import compiler
 from tests.cpu_kv8 import Cache, call
-from tests.kv8_cases import assert_fine, outlier_queries
+from tests.kv8_cases import assert_fine, opposed_values, outlier_queries
 
 FORMATS = [kv8.INT8, kv8.E4M3]
 
@@ -66,3 +66,13 @@ def test_one_large_query_channel(exe, fmt, large, small, k_size, digits):
     (st, bits, _, out), = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)
     assert (st, bits) == (0, 0)
     assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq", range(2, 17, 2))
+def test_values_that_cancel(exe, fmt, hq):
+    """Weights keep fp32's bits on their way to the values."""
+    c, q = opposed_values(40, hq, fmt)
+    (st, bits, _, out), = call(exe, "decode", c, q=q, hq=hq, sm_scale=0.09)
+    assert (st, bits) == (0, 0)
+    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)

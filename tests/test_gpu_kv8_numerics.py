@@ -6,7 +6,7 @@ import torch
 import paper_2606_26666_amd as pkv
 from oracle import kv8
 from tests.cpu_kv8 import Cache
-from tests.kv8_cases import assert_decode, assert_fine
+from tests.kv8_cases import assert_decode, assert_fine, opposed_values
 from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros
 
 pytestmark = pytest.mark.gpu
@@ -51,3 +51,10 @@ def test_columns_of_a_head_agree(fmt, hq):
     c = Cache([5] * 4096, 2, fmt, seed=3)
     q = np.random.default_rng(8).standard_normal((4096, hq, 128)).astype(np.float16)
     assert_decode(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq", range(2, 17, 2))
+def test_values_that_cancel(fmt, hq):
+    c, q = opposed_values(400, hq, fmt)
+    assert_fine(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)
