@@ -360,8 +360,9 @@ int pkv_stream_read_pages(const uint16_t* k_cache, const uint16_t* v_cache, int3
  * max_pages_per_row]; seq_lens int32 [B]; ws a workspace set up by pkv_workspace_init for (B, Hkv),
  * whose error word takes the device error bits (pkv_check_device_status). Two rows' tables may name
  * the same page (a shared prefix) as long as no call appends to it for more than one of them.
- * Calls on one stream may share a workspace; captured graphs too, replayed one after another. One
- * workspace serves attention calls of one B and Hkv (its counters lie before its slots). */
+ * Calls on one stream may share a workspace; captured graphs too, replayed one after another. A
+ * workspace made and initialised for the largest B * Hkv and the largest Hq / Hkv of its attention calls
+ * serves them all (its counters are its start, its state slots its end). */
 #define PKV_KV8_INT8 0
 #define PKV_KV8_E4M3 1
 

@@ -546,7 +546,7 @@ def kv8_pool(num_pages: int, Hkv: int, d: int, device) -> torch.Tensor:
 
 
 class Kv8Buffers:
-    """The workspace of the pkv_kv8 calls for batches of B rows."""
+    """The workspace of the pkv_kv8 calls for batches of up to B rows."""
 
     def __init__(self, B: int, Hq: int, Hkv: int, d: int, device):
         self.B, self.Hq, self.Hkv, self.d = B, Hq, Hkv, d

@@ -27,6 +27,9 @@ int check_cache(const void* cache, int32_t num_pages, const int32_t* bt, int32_t
   return PKV_OK;
 }
 
+// State slots of an attention call, whatever its lengths.
+size_t slots_bytes(int G) { return (size_t)2 * kKv8MaxWorkgroups * slot_floats(G) * sizeof(float); }
+
 // A strided [tokens, heads, d] fp16 operand: rows of `heads * d` halves, 16-byte aligned.
 int check_rows(const void* p, int64_t stride, int64_t heads, int32_t d) {
   if (!p || !aligned(p, 16) || stride < heads * d || stride % 8 != 0) return PKV_ERR_INVALID_ARG;
@@ -56,7 +59,7 @@ size_t pkv_kv8_record_bytes(int32_t d) { return d == kHeadDim ? (size_t)kKv8Reco
 size_t pkv_kv8_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t d) {
   if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq / Hkv > kKv8MaxG || d != kHeadDim) return 0;
   if ((int64_t)B * Hkv > INT32_MAX) return 0;
-  return partials_offset(B, Hkv) + (size_t)2 * kKv8MaxWorkgroups * slot_floats(Hq / Hkv) * sizeof(float);
+  return partials_offset(B, Hkv) + slots_bytes(Hq / Hkv);
 }
 
 int pkv_kv8_append(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride, const int32_t* offsets,
@@ -97,6 +100,7 @@ int pkv_kv8_decode(const uint16_t* q, int64_t q_stride, const void* cache, int32
   char* w = static_cast<char*>(ws);
   Kv8DecodeArgs a;
   std::memset(&a, 0, sizeof(a));
+  a.G = Hq / Hkv;
   a.q = q;
   a.cache = static_cast<const uint8_t*>(cache);
   a.block_table = block_table;
@@ -104,14 +108,14 @@ int pkv_kv8_decode(const uint16_t* q, int64_t q_stride, const void* cache, int32
   a.out = out;
   a.err = reinterpret_cast<unsigned*>(w);
   a.counters = reinterpret_cast<int32_t*>(w + kWsHeaderBytes);
-  a.partials = reinterpret_cast<float*>(w + partials_offset(B, Hkv));
+  // The slots are the workspace's end, so that no batch's slots lie on the counters of one with more rows.
+  a.partials = reinterpret_cast<float*>(w + (ws_bytes - slots_bytes(a.G)) / 256 * 256);
   a.q_stride = q_stride;
   a.num_pages = num_pages;
   a.max_pages_per_row = max_pages_per_row;
   a.B = B;
   a.Hq = Hq;
   a.Hkv = Hkv;
-  a.G = Hq / Hkv;
   a.scale_log2 = (float)((double)sm_scale * 1.4426950408889634);  // log2(e)
   return from_hip(launch_kv8_decode(a, format, stream));
 }

@@ -12,7 +12,7 @@ namespace {
 struct Request {
   int32_t what, order, compute_units, calls;  // what: 0 append, 1 gather, 2 decode
   int32_t B, hq, hkv, num_pages, max_pages, format, tokens, has_offsets;
-  int32_t k_stride, v_stride, q_stride, workspace_rows;
+  int32_t k_stride, v_stride, q_stride, workspace_rows;  // of a batch that the workspace is for (0: this one)
   float sm_scale;
 };
 
@@ -51,12 +51,13 @@ int main(int argc, char** argv) {
     v = read<uint16_t>(f, (rows - 1) * r.v_stride + r.hkv * 128);
   }
   int32_t* offsets = r.has_offsets ? read<int32_t>(f, r.B + 1) : nullptr;
-  const size_t ws_bytes = pkv_kv8_workspace_size(r.B, r.hq, r.hkv, 128);
+  const int ws_rows = r.workspace_rows > 0 ? r.workspace_rows : r.B;
+  const size_t ws_bytes = pkv_kv8_workspace_size(ws_rows, r.hq, r.hkv, 128);
   char* ws = guarded(ws_bytes);
   std::memset(ws, 0xFF, ws_bytes);
   uint16_t* out = (uint16_t*)guarded(2 * qn);
   FILE* g = std::fopen(argv[2], "wb");
-  if (!g || pkv_workspace_init(ws, ws_bytes, r.B, r.hkv, nullptr) != PKV_OK) return 2;
+  if (!g || pkv_workspace_init(ws, ws_bytes, ws_rows, r.hkv, nullptr) != PKV_OK) return 2;
   for (int c = 0; c < r.calls; ++c) {
     std::memset(out, 0xFF, 2 * qn);
     int st;
@@ -71,7 +72,7 @@ int main(int argc, char** argv) {
                           r.sm_scale, out, ws, ws_bytes, nullptr);
     uint32_t bits = 0;
     int32_t left = 0;  // completion counters that are not zero
-    for (int i = 0; i < r.B * r.hkv; ++i) left += reinterpret_cast<int32_t*>(ws + pkv::kWsHeaderBytes)[i] != 0;
+    for (int i = 0; i < ws_rows * r.hkv; ++i) left += reinterpret_cast<int32_t*>(ws + pkv::kWsHeaderBytes)[i] != 0;
     pkv_check_device_status(ws, nullptr, &bits);
     int32_t head[3] = {st, (int32_t)bits, left};
     std::fwrite(head, 4, 3, g);
