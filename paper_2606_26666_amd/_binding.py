@@ -464,7 +464,7 @@ def _explain_offsets(offsets, B: int):
 
 
 # The checks of these calls are one expression each, since a call is often shorter than a dozen
-# microseconds; where it fails, the _explain functions say what is wrong.
+# microseconds; where it fails, the call is refused, and the _explain functions say what is wrong.
 
 def _move(k, v, cache, block_table, seq_lens, ws, offsets, stream):
     """Checks of append and gather; (k, v, strides, offsets, tokens) and (num_pages, table, ...) as
@@ -486,6 +486,7 @@ def _move(k, v, cache, block_table, seq_lens, ws, offsets, stream):
         _explain_cache(cache, block_table, seq_lens, ws, d, hkv)
         _explain_offsets(offsets, B)
         _one_device(stream, k=k, v=v, cache=cache, block_table=block_table, seq_lens=seq_lens, offsets=offsets, ws=ws)
+        raise ValueError("the call's tensors do not fit together")
     return ((k.data_ptr(), v.data_ptr(), ks, vs, 0 if offsets is None else offsets.data_ptr(), tokens),
             (cache.data_ptr(), pool[0], block_table.data_ptr(), table[1], seq_lens.data_ptr()),
             (B, hkv, d), (ws.data_ptr(), ws.numel(), _stream(stream)))
@@ -531,6 +532,7 @@ def pkv_kv8_decode(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tens
         if table[0] != B or out.shape != shape:
             raise ValueError("q and out must be [B, Hq, d] with the block table's B")
         _one_device(stream, q=q, cache=cache, block_table=block_table, seq_lens=seq_lens, out=out, ws=ws)
+        raise ValueError("the call's tensors do not fit together")
     st = lib().pkv_kv8_decode(q.data_ptr(), qs, cache.data_ptr(), pool[0], block_table.data_ptr(), table[1],
                               seq_lens.data_ptr(), B, hq, pool[1], d, format, sm_scale, out.data_ptr(), ws.data_ptr(),
                               ws.numel(), _stream(stream))
