@@ -108,8 +108,9 @@ void run(const void* kernel_at, dim3 grid, dim3 block, const std::function<void(
   while ((int)stacks.size() < (int)block.x)
     stacks.push_back((char*)mmap(nullptr, kStack, PROT_READ | PROT_WRITE, MAP_PRIVATE | MAP_ANONYMOUS, -1, 0));
   uint64_t rng = order * 0x9E3779B97F4A7C15ull + 1;
-  for (unsigned b = 0; b < grid.x; ++b) {
-    block_idx = dim3(b);
+  const unsigned last = last_workgroup >= 0 && last_workgroup < (int)grid.x ? last_workgroup : grid.x - 1;
+  for (unsigned i = 0; i < grid.x; ++i) {
+    block_idx = dim3(i < last ? i : i + 1 < grid.x ? i + 1 : last);
     waves.assign(nw, Wave());
     for (unsigned t = 0; t < block.x; ++t) {
       Wave& w = waves[t / 64];

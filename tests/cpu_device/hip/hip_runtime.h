@@ -62,6 +62,8 @@ inline dim3 block_idx, block_dim, grid_dim;
 
 // 0: the lowest wave that can run, 1: the highest, otherwise a pseudo-random one (the seed)
 inline unsigned order = 0;
+// The workgroup that runs behind all others (-1: they run in order).
+inline int last_workgroup = -1;
 
 void run(const void* kernel_at, dim3 grid, dim3 block, const std::function<void()>& kernel);
 void wave_sync(const char* what);  // every live lane of the wave arrives

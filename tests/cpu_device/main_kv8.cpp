@@ -13,6 +13,7 @@ struct Request {
   int32_t what, order, compute_units, calls;  // what: 0 append, 1 gather, 2 decode
   int32_t B, hq, hkv, num_pages, max_pages, format, tokens, has_offsets;
   int32_t k_stride, v_stride, q_stride, workspace_rows;  // of a batch that the workspace is for (0: this one)
+  int32_t last_workgroup;
   float sm_scale;
 };
 
@@ -39,6 +40,7 @@ int main(int argc, char** argv) {
   if (!f || std::fread(&r, sizeof(r), 1, f) != 1) return 2;
   emu::order = (unsigned)r.order;
   emu::compute_units = r.compute_units;
+  emu::last_workgroup = r.last_workgroup;
   const size_t pool = (size_t)r.num_pages * r.hkv * pkv_kv8_record_bytes(128), qn = (size_t)r.B * r.hq * 128;
   uint8_t* cache = read<uint8_t>(f, pool);
   int32_t *table = read<int32_t>(f, (size_t)r.B * r.max_pages), *lens = read<int32_t>(f, r.B);

@@ -66,19 +66,21 @@ class Cache:
 
 
 def call(exe, what, cache, *, lens=None, bt=None, q=None, k=None, v=None, offsets=None, tokens=0, strides=None, hq=None,
-         order=ASCENDING, compute_units=2, calls=1, sm_scale=1.0, num_pages=None, workspace_rows=0):
+         order=ASCENDING, compute_units=2, calls=1, sm_scale=1.0, num_pages=None, workspace_rows=0,
+         last_workgroup=-1):
     """[(status, error bits, counters left, array or pair)] of each call; k and v are [tokens, stride]
     flat arrays for append, strides (k, v) for append and gather, (q,) for decode. workspace_rows: the batch
-    that the workspace was made for (0: this one)."""
+    that the workspace was made for (0: this one). last_workgroup: the one that runs behind all others (-1: in order)."""
     B, hkv = cache.B, cache.hkv
     hq = hq or hkv
     lens = cache.lens if lens is None else np.asarray(lens, dtype=np.int32)
     bt = cache.bt if bt is None else np.ascontiguousarray(bt, dtype=np.int32)
     strides = strides or ((hkv * 128,) * 2 if what != "decode" else (hq * 128,))
     ks, vs = strides if what != "decode" else (0, 0)
-    head = struct.pack("<16if", ("append", "gather", "decode").index(what), order, compute_units, calls, B, hq, hkv,
+    head = struct.pack("<17if", ("append", "gather", "decode").index(what), order, compute_units, calls, B, hq, hkv,
                        cache.num_pages if num_pages is None else num_pages, bt.shape[1], cache.fmt, tokens,
-                       offsets is not None, ks, vs, strides[0] if what == "decode" else 0, workspace_rows, sm_scale)
+                       offsets is not None, ks, vs, strides[0] if what == "decode" else 0, workspace_rows,
+                       last_workgroup, sm_scale)
     parts = [cache.pool, bt, lens]
     if what == "decode":
         parts.append(q.reshape(-1)[:(B - 1) * strides[0] + hq * 128])

@@ -1,4 +1,4 @@
-"""One workspace for batches of several sizes, on the GPU."""
+"""One workspace for batches of several sizes, and merges of many workgroups' states, on the GPU."""
 import numpy as np
 import pytest
 import torch
@@ -26,3 +26,14 @@ def test_batches_of_several_sizes_share_a_workspace(fmt):
             assert torch.equal(out, w)
             assert pkv.pkv_check_device_status(many.bufs.ws) == 0
             assert not many.bufs.ws[256:256 + 4 * 600 * 4].any()  # every counter of the largest batch is zero
+
+
+@pytest.mark.parametrize("hq", [1, 4, 7])
+@pytest.mark.parametrize("lens", [[40_000], [70_000], [9_000, 7_000], [33_000, 0, 30_000]])
+def test_merges_of_many_workgroups(lens, hq):
+    """One KV head: up to 256 workgroups' states for a row."""
+    d = Device(Cache(lens, 1, pkv.PKV_KV8_INT8, seed=2), hq)
+    out = d.decode()
+    d.check(out)
+    for _ in range(5):  # whichever workgroup merges
+        assert torch.equal(d.decode(), out)
