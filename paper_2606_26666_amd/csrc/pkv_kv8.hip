@@ -20,7 +20,10 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 
-constexpr int kNt = 2;    // cache-policy operand of a buffer access: non-temporal (a call reads each record once)
+// Cache-policy operand of a buffer access: non-temporal. A call reads a record once unless rows share pages, which
+// it cannot tell beforehand: 64 rows of 4160 tokens 98 us against 110 with the default policy, 32 of 16512
+// 182 against 201; with all but the last 64 or 128 tokens shared 78 against 76 and 145 against 135.
+constexpr int kNt = 2;
 constexpr int kOutOfRange = (int)0x80000000u;  // an offset past any buffer: reads as zero, without memory
 constexpr int kSc1 = 16;  // cache-policy operand of a buffer access: coherent across the XCDs' L2 caches
 constexpr float kLowest = -3.0e38f;  // a finite start for running maxima: no infinity is subtracted from another

@@ -80,6 +80,17 @@ def outlier_queries(cache, hq, large, small, seed=3):
     return q
 
 
+def shared_prefix(fmt, seed=9):
+    """Rows whose tables name the same pages: a prefix of 37 pages, then pages of their own; the last row is the
+    prefix alone, cut inside a page, and names its first page twice."""
+    from tests.cpu_kv8 import Cache
+    c = Cache([700, 640, 593, 37 * 16, 400], 2, fmt, seed=seed)
+    c.bt[1:4, :37] = c.bt[0, :37]
+    c.bt[4, :25] = c.bt[0, :25]
+    c.bt[4, 20] = c.bt[4, 0]
+    return c
+
+
 def opposed_values(rows, hq, fmt, seed=6):
     """Rows of two tokens with nearly equal scores and opposed V: outputs are a small part of the values."""
     from tests.cpu_kv8 import Cache

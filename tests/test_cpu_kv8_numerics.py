@@ -7,7 +7,7 @@ from oracle import kv8
 from tests import cpu_kv8
 from tests.cpu_cases import compiler
 from tests.cpu_kv8 import Cache, call
-from tests.kv8_cases import assert_fine, opposed_values, outlier_queries
+from tests.kv8_cases import assert_decode, assert_fine, gathered, opposed_values, outlier_queries, shared_prefix
 
 FORMATS = [kv8.INT8, kv8.E4M3]
 
@@ -76,3 +76,27 @@ def test_values_that_cancel(exe, fmt, hq):
     (st, bits, _, out), = call(exe, "decode", c, q=q, hq=hq, sm_scale=0.09)
     assert (st, bits) == (0, 0)
     assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("units", [1, 3, 40])
+def test_rows_that_share_pages(exe, fmt, units):
+    """Attention and read-back over a shared prefix; each row's new token goes to a page of its own."""
+    c, r = shared_prefix(fmt), np.random.default_rng(2)
+    k, v = (r.standard_normal((5, 256)).astype(np.float16) for _ in "kv")
+    write = np.array([700, 640, 593, 0, 0])
+    (st, bits, _, pool), = call(exe, "append", c, lens=write, k=k, v=v, tokens=5, compute_units=units)
+    assert (st, bits) == (0, 0)
+    assert np.array_equal(pool, kv8.ref_append(c.pool, k.reshape(5, 2, 128), v.reshape(5, 2, 128), c.bt, write, fmt))
+    c.pool = pool
+    q = r.standard_normal((5, 8, 128)).astype(np.float16)
+    (st, bits, left, out), = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09, compute_units=units)
+    assert (st, bits, left) == (0, 0, 0)
+    assert_decode(out, q, c.pool, c.bt, c.lens, fmt, 0.09)
+    offs = np.concatenate([[0], np.cumsum(c.lens)])
+    n = int(offs[-1])
+    (st, bits, _, (ko, _)), = call(exe, "gather", c, k=np.zeros((n, 256), dtype=np.float16), v=np.zeros((n, 256), dtype=np.float16),
+                                   offsets=offs, tokens=n, compute_units=units)
+    assert (st, bits) == (0, 0)
+    for i in range(5):
+        assert np.array_equal(ko.reshape(n, 2, 128)[offs[i]:offs[i + 1]], gathered(c.pool, c.bt[i], 0, c.lens[i], fmt)[0])

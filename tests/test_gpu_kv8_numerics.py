@@ -6,7 +6,7 @@ import torch
 import paper_2606_26666_amd as pkv
 from oracle import kv8
 from tests.cpu_kv8 import Cache
-from tests.kv8_cases import assert_decode, assert_fine, opposed_values
+from tests.kv8_cases import assert_decode, assert_fine, gathered, opposed_values, shared_prefix
 from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +58,37 @@ def test_columns_of_a_head_agree(fmt, hq):
 def test_values_that_cancel(fmt, hq):
     c, q = opposed_values(400, hq, fmt)
     assert_fine(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("hq", [2, 8, 16])
+def test_rows_that_share_pages(fmt, hq):
+    c, r = shared_prefix(fmt), np.random.default_rng(2)
+    x = r.standard_normal((5, 4, 128)).astype(np.float16)
+    write = np.array([700, 640, 593, 0, 0], dtype=np.int32)
+    pool, ws = dev(c.pool), pkv.Kv8Buffers(5, 2, 2, 128, "cuda").ws
+    xd = dev(x)
+    pkv.pkv_kv8_append(xd[:, :2], xd[:, 2:], pool, dev(c.bt), dev(write), ws, format=fmt)
+    c.pool = kv8.ref_append(c.pool, x[:, :2], x[:, 2:], c.bt, write, fmt)
+    assert np.array_equal(pool.cpu().numpy(), c.pool)
+    q = r.standard_normal((5, hq, 128)).astype(np.float16)
+    assert_decode(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09)
+    offs = np.concatenate([[0], np.cumsum(c.lens)]).astype(np.int32)
+    k, v = (torch.zeros((int(offs[-1]), 2, 128), dtype=torch.float16, device="cuda") for _ in "kv")
+    pkv.pkv_kv8_gather(pool, dev(c.bt), dev(c.lens), k, v, ws, format=fmt, offsets=dev(offs))
+    for i in range(5):
+        for got, want in zip((k, v), gathered(c.pool, c.bt[i], 0, c.lens[i], fmt)):
+            assert np.array_equal(got[offs[i]:offs[i + 1]].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_one_token_of_each_row_is_read_back(fmt):
+    """Without offsets: each row's last token, and zeros for a row of length 0."""
+    c = Cache([1, 0, 16, 17, 30, 4, 700] * 9, 3, fmt, seed=2)
+    k, v = (torch.full((c.B, 3, 128), 7.0, dtype=torch.float16, device="cuda") for _ in "kv")
+    ws = pkv.Kv8Buffers(c.B, 3, 3, 128, "cuda").ws
+    pkv.pkv_kv8_gather(dev(c.pool), dev(c.bt), dev(c.lens), k, v, ws, format=fmt)
+    assert pkv.pkv_check_device_status(ws) == 0
+    for i, n in enumerate(c.lens.tolist()):
+        for got, want in zip((k, v), gathered(c.pool, c.bt[i], n - 1, n, fmt) if n else [np.zeros((1, 3, 128))] * 2):
+            assert np.array_equal(got[i].cpu().numpy(), want[0])
