@@ -371,7 +371,8 @@ size_t pkv_kv8_record_bytes(int32_t d);
 
 /* Bytes of workspace that pkv_kv8_decode needs: header, B * Hkv completion counters, and state
  * slots whose number does not depend on the lengths. Returns 0 on a bad argument (Hq / Hkv must be
- * 1 to 8). pkv_kv8_append and pkv_kv8_gather use the header only (256 bytes). */
+ * 1 to 8). pkv_kv8_append and pkv_kv8_gather use the header only and ask for its 256 bytes;
+ * pkv_workspace_init asks for header and counters, 512 bytes at least. */
 size_t pkv_kv8_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
 
 /* Quantise the last tokens of each row into its pages (one kernel).
@@ -385,8 +386,9 @@ size_t pkv_kv8_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
  *   tokens    rows of k and v (0: nothing is enqueued)
  *   cache     device, see above; only the named positions are written
  *   seq_lens  lengths after the append
- * A row whose length is out of range or below its token count sets PKV_DEVERR_SEQ_LEN, a page id
- * outside the pool PKV_DEVERR_PAGE_ID; the tokens concerned are not written. */
+ * A row with tokens in the call whose length is out of range or below their count (also a negative
+ * length without offsets) sets PKV_DEVERR_SEQ_LEN, a page id outside the pool PKV_DEVERR_PAGE_ID; the
+ * tokens concerned are not written. */
 int pkv_kv8_append(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride, const int32_t* offsets,
                    int32_t tokens, void* cache, int32_t num_pages, const int32_t* block_table,
                    int32_t max_pages_per_row, const int32_t* seq_lens, int32_t B, int32_t Hkv, int32_t d,

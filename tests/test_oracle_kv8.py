@@ -75,3 +75,21 @@ def test_attention_of_the_stored_values():
         k16[bt[0, t // 16], t % 16], v16[bt[0, t // 16], t % 16] = k[t], v[t]
     a, b = kv8.ref_decode8(q, pool, bt, lens, kv8.INT8, 0.3), ref_decode(q, k16, v16, bt, lens, 0.3)
     assert np.abs(a - b).max() < 1e-12 * np.abs(b).max()
+
+
+def test_error_of_a_value():
+    """At most half a step of its code: m / 254 in int8, the larger of 2^-4 |x| and 2^-10 m / 448 in e4m3, plus the
+    scale's rounding. Every fp16 magnitude up to m, for several m; each bound is reached to within 5%."""
+    every = np.arange(0x7C00, dtype=np.uint16).view(np.float16)
+    for m in (65504.0, 1.0, 3.0, 1.7, 0.0101, 2.0 ** -14):
+        m = float(np.float16(m))
+        x = every[every <= m]
+        x = np.concatenate([x, np.zeros(-len(x) % 127, dtype=np.float16)]).reshape(-1, 127)
+        x = np.concatenate([np.full((len(x), 1), m, dtype=np.float16), x], 1)
+        v = x.astype(np.float64)
+        for fmt, half in ((kv8.INT8, np.full_like(v, m / 254)), (kv8.E4M3, np.maximum(2.0 ** -4 * v, 2.0 ** -10 * m / 448))):
+            codes, s = kv8.quantise(x, fmt)
+            err = np.abs(kv8.VALUES[fmt][codes] * s[:, None].astype(np.float64) - v)
+            assert np.all(err <= half + 2.0 ** -24 * v), (m, fmt)
+            if m >= 1:
+                assert (err / half).max() > 0.95
