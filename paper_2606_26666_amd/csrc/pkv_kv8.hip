@@ -19,6 +19,7 @@ typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
+typedef unsigned short v2h __attribute__((ext_vector_type(2)));
 
 // Cache-policy operand of a buffer access: non-temporal. A call reads a record once unless rows share pages, which
 // it cannot tell beforehand: 64 rows of 4160 tokens 98 us against 110 with the default policy, 32 of 16512
@@ -51,20 +52,6 @@ __device__ __forceinline__ float across_rows(float x, F f) {
   asm volatile("" : "+v"(d));
   const auto t = __builtin_amdgcn_permlane32_swap(c, d, false, false);
   return f(as_f32((unsigned)t[0]), as_f32((unsigned)t[1]));
-}
-
-// Eight query values as bf16 high halves in a head's column h and low halves in column 15 - h (exact: fp16
-// has 11 bits). `there`: the column has a head.
-__device__ __forceinline__ b8v bf16_halves(v4u raw, bool there, int col) {
-  const h8v y = __builtin_bit_cast(h8v, raw);
-  b8v b;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float f = there ? (float)y[e] : 0.0f;
-    const __bf16 hi = (__bf16)f;
-    b[e] = col < 8 ? hi : (__bf16)(f - (float)hi);
-  }
-  return b;
 }
 
 template <typename F>
@@ -118,95 +105,101 @@ struct Int8 {
     return v2u{__builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302u), __builtin_amdgcn_perm(as_u32(d), as_u32(c), 0x07060302u)};
   }
   // Q.K in integers: K enters the matrix cores as it lies in memory, and a query vector as four
-  // balanced base-256 digits of x = q * 2^k, x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 with d3 in [-64, 64], the
-  // others in [-128, 127] (a digit's borders moved up by the digits below it). k is the largest up to 24
-  // with max|q| * 2^k <= 2^30. Where every x of the wave's heads is an integer (below 64 every fp16 is;
-  // above, one without bits below 2^-30 of its head's largest value, taken up to a power of two), the
-  // sums of digits times codes are exact, and two of them joined (d3 and d1, d2 and d0) rounded to fp32.
+  // balanced base-256 digits of x = q * 2^24, x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 with d3 in [-64, 64], the
+  // others in [-128, 127] (a digit's borders moved up by the digits below it). Below 64 any fp16 is such an
+  // integer of at most 30 bits. With larger values in a head, x = q * 2^k, k the largest with all below 2^30,
+  // and what that leaves of smaller values is two digits more, for which `low` says that there are any. So
+  // the sums of digits times codes are exact, whatever lies beside a large value; two or three of them
+  // are joined in fp32 (d3 and d1 in column h, d2 and d0 in column 15 - h).
   // A head's columns have to hold the same score to the last bit, since they hold parts of the same weight: they
   // are added before the scales come in, so that no product can be fused into the sum of one column and
   // not into the other's.
-  // Else the query goes in as bf16 halves and K is converted, as in E4m3, so that no bit of a small value
-  // is lost beside a large one.
-  // First operand: d3 in column h, d2 in column 15 - h; second: d1 and d0.
   struct Query {
-    v4u b[4];     // digits: [first, second][half]; else a quarter's bf16 each
-    float unit;   // 2^-k * scale, or the scale
-    float up;     // 2^8 in the columns of d3 and d1, 1 in the others
-    bool digits;
-    __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
-      unsigned top = 0;
+    v4u b[2][2];    // [d3 and d2, d1 and d0][half]
+    v4u b_low[2];
+    float unit;     // 2^-k * scale
+    float up;       // 2^8 in the columns of d3 and d1, 1 in the others
+    float up_low;   // of the digits beyond: up * 2^(k - 24)
+    bool low;
+    // Bytes of four digits: of x[i] + bias, the byte that `at` picks of a pair.
+    static __device__ __forceinline__ unsigned four(const unsigned* x, unsigned bias, unsigned at) {
+      return __builtin_amdgcn_perm(x[1] + bias, x[0] + bias, at) | __builtin_amdgcn_perm(x[3] + bias, x[2] + bias, at) << 16;
+    }
+    __device__ __forceinline__ void set(const v4u (&raw)[4], bool, int col, float scale) {
+      v4u r[4];
+      v2h most = {0, 0};
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j) {
+        r[j] = raw[j];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = max(top, max(raw[j][e] & 0x7FFFu, (raw[j][e] >> 16) & 0x7FFFu));
-      top = as_u32(across_rows(as_f32(top), [](float y, float z) { return as_f32(max(as_u32(y), as_u32(z))); }));
-      const bool finite = there && top < 0x7C00u;
-      const int k = min(24, 44 - (int)(top >> 10));  // |q| < 2^(exponent bits - 14)
-      const float raise = finite ? as_f32((unsigned)(127 + k) << 23) : 0.0f;
-      digits = true;
-      up = col < 8 ? 256.0f : 1.0f;
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(finite && k < 24) != 0, 0)) {
-        bool whole = true;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const h8v y = __builtin_bit_cast(h8v, raw[j]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = finite ? (float)y[e] * raise : 0.0f;
-            whole = whole && x == __builtin_truncf(x);
-          }
-        }
-        digits = __builtin_amdgcn_ballot_w64(!whole) == 0;
+        for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(v2h, raw[j][e] & 0x7FFF7FFFu));
       }
-      if (__builtin_expect(digits, 1)) {
-        unit = top < 0x7C00u ? as_f32((unsigned)(127 - k) << 23) * scale : __builtin_nanf("");
-        // A byte of x + bias is a digit: d3 that of 2^24 of x + 2^23 + 2^15 + 2^7, and so on.
-        const unsigned bias1 = col < 8 ? 0x808080u : 0x8080u, bias0 = col < 8 ? 0x80u : 0u;
-        const unsigned at1 = col < 8 ? 0x0C0C0703u : 0x0C0C0602u, at0 = col < 8 ? 0x0C0C0501u : 0x0C0C0400u;
+      // Bytes of a pair with nothing above: d3 that of 2^24 of x + 2^23 + 2^15 + 2^7, and so on.
+      const unsigned bias1 = col < 8 ? 0x808080u : 0x8080u, bias0 = col < 8 ? 0x80u : 0u;
+      const unsigned at1 = col < 8 ? 0x0C0C0703u : 0x0C0C0602u, at0 = col < 8 ? 0x0C0C0501u : 0x0C0C0400u;
+      unsigned top = max((unsigned)most.x, (unsigned)most.y);
+      up = col < 8 ? 256.0f : 1.0f;
+      float raise = 0x1p24f;
+      unit = 0x1p-24f * scale;
+      low = false;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top >= 0x5400u) != 0, 0)) {  // a value of 64 or more
+        top = as_u32(across_rows(as_f32(top), [](float y, float z) { return as_f32(max(as_u32(y), as_u32(z))); }));
+        const bool finite = top < 0x7C00u;
+        const int k = finite ? min(24, 44 - (int)(top >> 10)) : 24;  // |q| < 2^(exponent bits - 14)
+        raise = as_f32((unsigned)(127 + k) << 23);
+        unit = finite ? as_f32((unsigned)(127 - k) << 23) * scale : __builtin_nanf("");
+        up_low = up * as_f32((unsigned)(103 + k) << 23);
+        const float rest = as_f32((unsigned)(151 - k) << 23);
+        unsigned any = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const h8v y = __builtin_bit_cast(h8v, raw[j]);
+          r[j] = finite ? r[j] : v4u{0, 0, 0, 0};
+          const h8v y = __builtin_bit_cast(h8v, r[j]);
           unsigned x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = (unsigned)(int)(finite ? (float)y[e] * raise : 0.0f);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const unsigned* z = x + 4 * i;
-            b[j >> 1][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias1, z[0] + bias1, at1) |
-                                         __builtin_amdgcn_perm(z[3] + bias1, z[2] + bias1, at1) << 16;
-            b[2 + (j >> 1)][2 * (j & 1) + i] = __builtin_amdgcn_perm(z[1] + bias0, z[0] + bias0, at0) |
-                                               __builtin_amdgcn_perm(z[3] + bias0, z[2] + bias0, at0) << 16;
+          for (int e = 0; e < 8; ++e) {
+            const float f = (float)y[e] * raise;
+            x[e] = (unsigned)(int)((f - __builtin_truncf(f)) * rest);
+            any |= x[e];
           }
+          b_low[j >> 1][2 * (j & 1)] = four(x, bias0, at0);
+          b_low[j >> 1][2 * (j & 1) + 1] = four(x + 4, bias0, at0);
         }
-      } else {
-        unit = scale;
+        low = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(v4u, bf16_halves(raw[j], there, col));
+      for (int j = 0; j < 4; ++j) {  // (columns without a head hold the first one's)
+        const h8v y = __builtin_bit_cast(h8v, r[j]);
+        unsigned x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (unsigned)(int)((float)y[e] * raise);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          b[0][j >> 1][2 * (j & 1) + i] = four(x + 4 * i, bias1, at1);
+          b[1][j >> 1][2 * (j & 1) + i] = four(x + 4 * i, bias0, at0);
+        }
       }
     }
     __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
-      v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (__builtin_expect(!digits, 0)) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(load8<Int8>(k[j >> 1][2 * (j & 1)], k[j >> 1][2 * (j & 1) + 1]),
-                                                      __builtin_bit_cast(b8v, b[j]), x, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (x[i] + mirror16(x[i])) * (ks[i] * unit);
-        return x;
-      }
       v4i c = {0, 0, 0, 0}, c0 = {0, 0, 0, 0};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[half]), c, 0, 0, 0);
-        c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[2 + half]), c0, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[0][half]), c, 0, 0, 0);
+        c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b[1][half]), c0, 0, 0, 0);
+      }
+      v4f x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf((float)c[i], 65536.0f * up, (float)c0[i] * up);
+      if (__builtin_expect(low, 0)) {
+        v4i d = {0, 0, 0, 0};
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          d = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, k[half]), __builtin_bit_cast(v4i, b_low[half]), d, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf((float)d[i], up_low, x[i]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float y = __builtin_fmaf((float)c[i], 65536.0f * up, (float)c0[i] * up);
-        x[i] = (y + mirror16(y)) * (ks[i] * unit);
-      }
+      for (int i = 0; i < 4; ++i) x[i] = (x[i] + mirror16(x[i])) * (ks[i] * unit);
       return x;
     }
   };
@@ -226,14 +219,23 @@ struct E4m3 {
     return v2u{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
   }
-  // Q.K in bf16: K exactly, a query's halves (exact); the two columns' sums are added.
+  // Q.K in bf16: K exactly, a query value as its bf16 high half in column h and low half in column
+  // 15 - h (exact: fp16 has 11 bits); the two columns' sums are added.
   struct Query {
     b8v b[4];
     float unit;
     __device__ __forceinline__ void set(const v4u (&raw)[4], bool there, int col, float scale) {
       unit = scale;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = bf16_halves(raw[j], there, col);
+      for (int j = 0; j < 4; ++j) {
+        const h8v y = __builtin_bit_cast(h8v, raw[j]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f = there ? (float)y[e] : 0.0f;
+          const __bf16 hi = (__bf16)f;
+          b[j][e] = col < 8 ? hi : (__bf16)(f - (float)hi);
+        }
+      }
     }
     __device__ __forceinline__ v4f scores(const v4u (&k)[2], v4f ks) const {
       v4f x = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -32,14 +32,14 @@ def assert_decode(out, q, pool, bt, lens, fmt, sm_scale, what=""):
     assert np.all(err <= tol), (what, float((err / tol).max()), float(np.nanmax(err)))
 
 
-def fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores):
+def fine_bound(q, pool, bt, lens, fmt, sm_scale):
     """(reference, bound) [B, Hq, 128] for rows of at most 32 tokens, whose weights are formed under one
     maximum, with no factor that real errors cannot reach. With S = |scale| sum|q k| of a token:
     - a score s: the scale to fp32 and times log2(e), that times the query's unit and the K scale, and the sum
-      times that, and the sum of its two halves: five roundings, 2^-24 each. The halves themselves: in integers
-      (exact_scores) the query x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 is taken as d3, d1 and d2, d0; each half's sum is
-      rounded once, and |2^24 d3 + 2^8 d1| + |2^16 d2 + d0| <= 3.01 |x| (the second sum is at most 2^23 + 2^7, and
-      d3 = 0 unless |x| >= 2^23 - 2^15 - 2^7): 3.1 S of 2^-24. In bf16 each of 129
+      times that, and the sum of its two halves: five roundings, 2^-24 each. The halves themselves: in int8 the query
+      x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 is taken as d3, d1 and d2, d0, whose exact sums are joined in one rounding each,
+      and in one more where there are digits beyond, and |2^24 d3 + 2^8 d1| + |2^16 d2 + d0| <= 3.01 |x| (the second
+      sum is at most 2^23 + 2^7, and d3 = 0 unless |x| >= 2^23 - 2^15 - 2^7): 6.1 S of 2^-24. In e4m3 each of 129
       additions is off by at most 2^-23 of S.
     - a weight, relatively: the error of s; s - max rounded, 2^-24 of it; exp2 2^-23.
     - a weight's error d moves the output by p d |v - o| (p: the weight over the weights' sum, o: the output).
@@ -59,14 +59,14 @@ def fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores):
             s, size = sm_scale * (k @ x), abs(sm_scale) * (np.abs(k) @ np.abs(x))
             p = np.exp(s - s.max())
             p /= p.sum()
-            d = 2.0 ** -24 * (5 * np.abs(s) + (3.1 if exact_scores else 2 * 129) * size + np.abs(s - s.max())) + 2.0 ** -23
+            d = 2.0 ** -24 * (5 * np.abs(s) + (6.1 if fmt == kv8.INT8 else 2 * 129) * size + np.abs(s - s.max())) + 2.0 ** -23
             tol[i, h] += (p * d) @ np.abs(v - ref[i, h]) + (p @ np.abs(v)) * (2.0 ** -23 + 3 * n * 2.0 ** -23)
             tol[i, h] += np.abs(ref[i, h]) * ((n + 4) * 2.0 ** -24 + 2.0 ** -22)
     return ref, tol
 
 
-def assert_fine(out, q, pool, bt, lens, fmt, sm_scale, exact_scores):
-    ref, tol = fine_bound(q, pool, bt, lens, fmt, sm_scale, exact_scores)
+def assert_fine(out, q, pool, bt, lens, fmt, sm_scale):
+    ref, tol = fine_bound(q, pool, bt, lens, fmt, sm_scale)
     err = np.abs(np.asarray(out, dtype=np.float64) - ref)
     assert np.all(err <= tol), (float((err / tol).max()), float(np.nanmax(err)))
 

@@ -42,11 +42,10 @@ def test_zeros_of_both_signs(exe, fmt, offsets):
     assert np.array_equal(pool, kv8.ref_append(c.pool, x, x[::-1], c.bt, c.lens, fmt, offsets))
 
 
-# The large channel, the size of the others (2: multiples of 1/64) and of K, and whether the int8 scores are
-# sums of integers: 30 bits from the large channel down reach to 2^-14 (60000), 2^-16 (16000), 2^-21 (300) or, below
-# 64, to the last bit of fp16.
-OUTLIERS = [(60000, 2.0, 1, True), (16000, 2.0, 1, True), (40, 1.0, 1, True), (60000, 0.01, 100, False), (300, 1e-4, 2000, False),
-            (6e-5, 3e-7, 30000, True), (60000, 0, 1, True)]
+# The large channel, the size of the others (2: multiples of 1/64) and of K. Below 64 the int8 scores' four digits reach
+# to the last bit of fp16; 30 bits from a larger value down to 2^-14 (60000, 65504), 2^-16 (16000) or 2^-21 (300).
+OUTLIERS = [(60000, 2.0, 1), (16000, 2.0, 1), (40, 1.0, 1), (63.97, 1.0, 1), (64, 1.0, 1), (60000, 0.01, 100), (300, 1e-4, 2000),
+            (-65504, 1.0, 1), (6e-5, 3e-7, 30000), (60000, 0, 1)]
 
 
 def outlier_case(fmt, large, small, k_size):
@@ -60,12 +59,12 @@ def outlier_case(fmt, large, small, k_size):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("large,small,k_size,digits", OUTLIERS)
-def test_one_large_query_channel(exe, fmt, large, small, k_size, digits):
+@pytest.mark.parametrize("large,small,k_size", OUTLIERS)
+def test_one_large_query_channel(exe, fmt, large, small, k_size):
     c, q = outlier_case(fmt, large, small, k_size)
     (st, bits, _, out), = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)
     assert (st, bits) == (0, 0)
-    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)
+    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -75,7 +74,7 @@ def test_values_that_cancel(exe, fmt, hq):
     c, q = opposed_values(40, hq, fmt)
     (st, bits, _, out), = call(exe, "decode", c, q=q, hq=hq, sm_scale=0.09)
     assert (st, bits) == (0, 0)
-    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)
+    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -100,3 +99,17 @@ def test_rows_that_share_pages(exe, fmt, units):
     assert (st, bits) == (0, 0)
     for i in range(5):
         assert np.array_equal(ko.reshape(n, 2, 128)[offs[i]:offs[i + 1]], gathered(c.pool, c.bt[i], 0, c.lens[i], fmt)[0])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_a_query_that_is_not_finite_reaches_its_head_only(exe, fmt, bad):
+    c, q = outlier_case(fmt, 300, 1.0, 1)
+    q[:, 2, 77] = bad
+    (st, bits, _, out), = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)
+    live = c.lens > 0
+    assert (st, bits) == (0, 0) and np.isnan(out[live, 2]).all() and not out[~live].any()
+    keep = [h for h in range(8) if h != 2]
+    q[:, 2, 77] = 0
+    want = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)[0][3]
+    assert np.array_equal(out[:, keep], want[:, keep])

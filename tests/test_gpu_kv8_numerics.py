@@ -37,10 +37,10 @@ def attend(c, q, hq):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("large,small,k_size,digits", OUTLIERS)
-def test_one_large_query_channel(fmt, large, small, k_size, digits):
+@pytest.mark.parametrize("large,small,k_size", OUTLIERS)
+def test_one_large_query_channel(fmt, large, small, k_size):
     c, q = outlier_case(fmt, large, small, k_size)
-    assert_fine(attend(c, q, 8), q, c.pool, c.bt, c.lens, fmt, 0.09, digits and fmt == kv8.INT8)
+    assert_fine(attend(c, q, 8), q, c.pool, c.bt, c.lens, fmt, 0.09)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -57,7 +57,7 @@ def test_columns_of_a_head_agree(fmt, hq):
 @pytest.mark.parametrize("hq", range(2, 17, 2))
 def test_values_that_cancel(fmt, hq):
     c, q = opposed_values(400, hq, fmt)
-    assert_fine(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09, fmt == kv8.INT8)
+    assert_fine(attend(c, q, hq), q, c.pool, c.bt, c.lens, fmt, 0.09)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -92,3 +92,15 @@ def test_one_token_of_each_row_is_read_back(fmt):
     for i, n in enumerate(c.lens.tolist()):
         for got, want in zip((k, v), gathered(c.pool, c.bt[i], n - 1, n, fmt) if n else [np.zeros((1, 3, 128))] * 2):
             assert np.array_equal(got[i].cpu().numpy(), want[0])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_a_query_that_is_not_finite_reaches_its_head_only(fmt, bad):
+    c, q = outlier_case(fmt, 300, 1.0, 1)
+    q[:, 2, 77] = bad
+    out, live = attend(c, q, 8), c.lens > 0
+    assert np.isnan(out[live, 2]).all() and not out[~live].any()
+    keep = [h for h in range(8) if h != 2]
+    q[:, 2, 77] = 0
+    assert np.array_equal(out[:, keep], attend(c, q, 8)[:, keep])
