@@ -522,29 +522,33 @@ __global__ __launch_bounds__(kMoveWaves * 64) void move_kernel(Kv8MoveArgs a, in
 // own. The record's V layout gives each lane its four tokens of eight dims as whole dwords, and K is
 // token-major: codes go from HBM into registers and from there into the matrix cores, without LDS.
 //
-// What bounds it: reading the records. 32 rows of up to 32 K tokens (928 MB) take 151 us, 6.2 TB/s of
-// the 6.9 that a large read reaches; without any arithmetic the same loads take 149. Beyond the read a
-// call has some 13 us that do not depend on its size: the start of the waves and their first ids and
-// pages (5-6), and at the end the slowest wave, the join in the workgroup, and the states' way through
-// memory to the last workgroup and back (6). The vector ALU is busy for 40% of the time, the matrix
-// cores for 8%. Short rows are bound by the chain of a pair (about 1.4 us), not by bytes. Wave priorities by
-// progress and workgroups numbered by XCD were within 4% either way; four waves of a workgroup instead of
-// eight were slower (64 rows of up to 2048 tokens 55 us against 52), and so were two pairs at a time under
-// one maximum (rows of 16-1024 tokens at G = 8 73 us against 67: every odd pair costs two).
+// What bounds it: reading the records. 32 rows of up to 32 K tokens (928 MB) take 153 us, 6.1 TB/s of
+// the 6.9 that a large read reaches; without any arithmetic the same loads take 149. What is left over in
+// smaller calls is 13 us at 69 MB and 13-21 at 212-309 MB: the start of the waves with their first ids and
+// pages, the spread of the waves' ends, the join, and states that go through memory to the last workgroup. (A
+// call that has neither long rows nor a merge takes 8 in all.) The vector ALU is busy for 43% of the time, the
+// matrix cores for 11%. Short rows are bound by the chain of a pair (about 1.6 us: one row of 512 tokens, two
+// pairs a wave, 11.0, of 1024 14.2), not by bytes. Wave priorities by progress and workgroups numbered by XCD
+// were within 4% either way; four waves of a workgroup instead of eight were slower (64 rows of 128-4096 tokens
+// 55 us against 52), and so were two pairs at a time under one maximum (rows of 16-1024 tokens at G = 8 73 us
+// against 67: every odd pair costs two).
 constexpr int kLogW = 3, W = 1 << kLogW;  // waves of a workgroup
 constexpr int kSegment = 1;  // units of a segment beyond its pairs
 // Up to so many pairs of the longest row (half of them unless the waves have several segments each)
 // a wave takes whole segments: what it has more or less than others costs less than states that
-// meet (Hkv = 8, 256 rows of 10-60 tokens 22.5 -> 13.9 us, of 60-130 26.9 -> 22.7, of 100-250 31.6 ->
-// 28.3, of 100-400 36.8 -> 35.4; Hkv = 32, 64 rows of 100-300 30.3 -> 26.7). Beyond it does not (512 rows
-// of 100-600 tokens 78 -> 87).
+// meet (int8, 8 KV heads: 256 rows of 10-60 tokens 20.7 -> 14.8 us, of 60-130 27.1 -> 24.4, of 100-250
+// 31.4 -> 30.0; 32 KV heads, 64 rows of 100-300 32.1 -> 29.8). Towards the limit it goes either way (256 rows
+// of 100-400 in int8 37.5 -> 39.2, in e4m3 37.8 -> 36.6; 32 KV heads, 128 rows of 100-500 in int8 69.0 -> 73.6,
+// in e4m3 69.8 -> 70.1), beyond it does not pay (512 rows of 100-600 in int8 80 -> 91, in e4m3 78 -> 88).
 constexpr int kWhole = 16;
 constexpr int kIdPairs = 32;  // page pairs whose ids a wave holds (one id a lane)
 // Pairs of the longest row times the segments per workgroup, up to which workgroups have segments of
-// their own: four pairs a wave, whose chain is as long as that of a merge over workgroups (one row of
-// 1024 tokens 14.5 us, of 1100 over many workgroups 14.2; Hkv = 8, 64 rows of 100-300 tokens, two segments
-// a workgroup, 14.0 against 17.2, of 100-500 15.6 against 20.6; 32 KV heads, 16 rows of 100-500 15.8 against
-// 20.4). With two pairs or one a segment a wave for each is faster (64 rows of 20-60 8.6 against 9.6).
+// their own: four pairs a wave. With one segment a workgroup that is where the chain is as long as that
+// of a merge over workgroups (int8, one row of 1024 tokens 14.2 us either way, of 512 11.0 against 14.4); with
+// two it pays throughout (8 KV heads, 64 rows of 100-300 tokens 14.5 against 18.2, of 100-500 16.1 against 21.0;
+// 32 KV heads, 16 rows of 100-500 15.8 against 21.0). With four it would also beyond, at eight pairs a wave (128
+// rows of 100-500 24.8 against 28.8; 32 KV heads, 32 rows of 100-400 21.7 against 25.5). With two pairs or one
+// a segment a wave for each is faster (64 rows of 20-60 9.0 against 9.6), or as fast (128 of 20-60 11.2 against 10.8).
 constexpr int kOwn = 32;
 static_assert(kOwn <= kIdPairs && W == 8, "the ids fetched ahead are a segment's first");
 
