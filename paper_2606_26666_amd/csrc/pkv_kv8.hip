@@ -110,7 +110,8 @@ struct Int8 {
   // integer of at most 30 bits. With larger values in a head, x = q * 2^k, k the largest with all below 2^30,
   // and what that leaves of smaller values is two digits more, for which `low` says that there are any. So
   // the sums of digits times codes are exact, whatever lies beside a large value; two or three of them
-  // are joined in fp32 (d3 and d1 in column h, d2 and d0 in column 15 - h).
+  // are joined in fp32 (d3 and d1 in column h, d2 and d0 in column 15 - h). A channel of 100 in every head: one row
+  // of 77 tokens 8.6 us against 8.0, of 32 K 24.7 against 24.0, larger calls the same.
   // A head's columns have to hold the same score to the last bit, since they hold parts of the same weight: they
   // are added before the scales come in, so that no product can be fused into the sum of one column and
   // not into the other's.

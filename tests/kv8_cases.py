@@ -34,7 +34,8 @@ def assert_decode(out, q, pool, bt, lens, fmt, sm_scale, what=""):
 
 def fine_bound(q, pool, bt, lens, fmt, sm_scale):
     """(reference, bound) [B, Hq, 128] for rows of at most 32 tokens, whose weights are formed under one
-    maximum, with no factor that real errors cannot reach. With S = |scale| sum|q k| of a token:
+    maximum, with no factor that real errors cannot reach (decode_bound, for rows of any length, grants the weights
+    8 bits less than they have, and scores the worst order of sums). With S = |scale| sum|q k| of a token:
     - a score s: the scale to fp32 and times log2(e), that times the query's unit and the K scale, and the sum
       times that, and the sum of its two halves: five roundings, 2^-24 each. The halves themselves: in int8 the query
       x = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0 is taken as d3, d1 and d2, d0, whose exact sums are joined in one rounding each,

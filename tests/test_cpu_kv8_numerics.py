@@ -113,3 +113,22 @@ def test_a_query_that_is_not_finite_reaches_its_head_only(exe, fmt, bad):
     q[:, 2, 77] = 0
     want = call(exe, "decode", c, q=q, hq=8, sm_scale=0.09)[0][3]
     assert np.array_equal(out[:, keep], want[:, keep])
+
+
+def some_heads_large(fmt, g):
+    """One head with a large channel, one with values just below 64, the others ordinary."""
+    c = Cache([31, 1, 0, 32, 17], 2, fmt, seed=15)
+    q = outlier_queries(c, 2 * g, 1.0, 1.0)
+    q[:, 0, 5] = 1000
+    q[:, 0, 9] = 2.0 ** -13 + 2.0 ** -23
+    q[:, -1, 5] = 63.96875
+    return c, q
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("g", range(1, 9))
+def test_a_large_channel_of_one_head(exe, fmt, g):
+    c, q = some_heads_large(fmt, g)
+    (st, bits, _, out), = call(exe, "decode", c, q=q, hq=2 * g, sm_scale=0.09)
+    assert (st, bits) == (0, 0)
+    assert_fine(out, q, c.pool, c.bt, c.lens, fmt, 0.09)

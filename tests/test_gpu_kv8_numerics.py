@@ -7,7 +7,7 @@ import paper_2606_26666_amd as pkv
 from oracle import kv8
 from tests.cpu_kv8 import Cache
 from tests.kv8_cases import assert_decode, assert_fine, gathered, opposed_values, shared_prefix
-from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros
+from tests.test_cpu_kv8_numerics import FORMATS, OUTLIERS, outlier_case, signed_zeros, some_heads_large
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,10 @@ def test_a_query_that_is_not_finite_reaches_its_head_only(fmt, bad):
     keep = [h for h in range(8) if h != 2]
     q[:, 2, 77] = 0
     assert np.array_equal(out[:, keep], attend(c, q, 8)[:, keep])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("g", range(1, 9))
+def test_a_large_channel_of_one_head(fmt, g):
+    c, q = some_heads_large(fmt, g)
+    assert_fine(attend(c, q, 2 * g), q, c.pool, c.bt, c.lens, fmt, 0.09)
